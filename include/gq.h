@@ -330,6 +330,42 @@ int32_t gq_cd_cycles(const float *W, float *W_hat, uint8_t *Q, const float *code
 size_t gq_cd_workspace_bytes(int64_t d_in, int64_t d_out, int32_t g);
 
 /*
+ * The end loss (the loss that Section 3 takes its gradients of): log probabilities of given tokens, with entropies and the
+ * highest alternatives.  For every row x of the logits, with m = max_j x_j and L = log sum_j exp(x_j - m),
+ *     logp    = x_t - m - L            (t = the row's target)
+ *     entropy = -sum_j p_j log p_j,  p_j = exp(x_j - m - L)
+ *
+ *   logits     [n, ld] of `dtype` (enum gq_dtype), aligned to its element size, ld >= vocab.  Entries may be -inf (tokens that are
+ *              ruled out): p = 0.  A row of nothing but -inf has m = -inf, L = 0, entropy 0, log probabilities -inf.  A NaN or
+ *              +inf in a row makes its results NaN.
+ *   n, vocab   n >= 0 (0 is a no-op), 1 <= vocab <= 2^30, 8 n < 2^31
+ *   targets    int64 [n] or NULL (then logp is NULL too).  A target outside [0, vocab) is a token that does not count: its
+ *              logp is 0.
+ *   top        0 .. 32 and at most vocab: how many alternatives
+ *   logp       fp32 [n], entropy fp32 [n], stats fp32 [n, 2]: m and L of every row
+ *   top_logp   fp32 [n, top], top_ids int32 [n, top]: the highest log probabilities in falling order, equal logits by rising
+ *              index (NULL if top is 0).  Where fewer than `top` logits are numbers the rest is NaN with index -1.
+ * Sums are fp32.  One launch; few rows are split over up to eight CTAs each.  Results are bit-reproducible.
+ */
+int32_t gq_token_logprobs(const void *logits, int32_t dtype, int64_t n, int64_t vocab, int64_t ld, const int64_t *targets,
+                          int32_t top, float *logp, float *entropy, float *stats, float *top_logp, int32_t *top_ids,
+                          void *stream);
+
+/*
+ * Its gradient in the logits, where a saliency step's backward pass starts:
+ *     d_logits[j] = d_logp (1[j = t] - p_j) - d_entropy p_j (log p_j + entropy)
+ *
+ *   logits, dtype, n, vocab, ld, targets, stats, entropy     as given to and left by gq_token_logprobs
+ *   d_logp     fp32 [n] or NULL (with targets); d_entropy fp32 [n] or NULL (entropy may then be NULL); one of them is given
+ *   d_logits   [n, ld_d] of `dtype`, aligned to its element size, ld_d >= vocab, rounded once at the end
+ * Rows whose token does not count, or with d_logp = 0, and without an entropy gradient get zeros whatever their logits hold;
+ * so does a row of nothing but -inf.
+ */
+int32_t gq_token_logprobs_grad(const void *logits, int32_t dtype, int64_t n, int64_t vocab, int64_t ld, const int64_t *targets,
+                               const float *stats, const float *entropy, const float *d_logp, const float *d_entropy,
+                               void *d_logits, int64_t ld_d, void *stream);
+
+/*
  * Synchronises `stream`, then returns and clears the first device-side error recorded on the
  * current device since the last gq_check (GQ_OK if none).  A pipeline wait inside a kernel that
  * exceeds its time budget (2 s by default; environment variable GQ_WAIT_BUDGET_MS) makes the
@@ -417,7 +453,8 @@ enum gq_kernel_id {
     GQ_KERNEL_CB_FOLD = 11,    /* codebook step: sums over the rows of each level, m x m solves */
     GQ_KERNEL_CB_AUX = 12,     /* codebook step: splits, transposes, one-hot columns, W_hat */
     GQ_KERNEL_EXCHANGE = 13,   /* token-sharded accumulation: reduce / gather of blocks of H over peer memory */
-    GQ_KERNEL_COUNT = 14
+    GQ_KERNEL_SCORE = 14,      /* log probabilities of tokens and their gradient         */
+    GQ_KERNEL_COUNT = 15
 };
 
 /*

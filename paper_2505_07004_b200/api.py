@@ -26,11 +26,12 @@ EXPORTS = (
     "gq_kernel_timing_enable", "gq_kernel_timing_read", "gq_objective_noalloc", "gq_cd_cycles", "gq_cd_workspace_bytes",
     "gq_selftest_wait_timeout", "gq_codebook_update", "gq_codebook_workspace_bytes",
     "gq_hessian_reduce_share", "gq_hessian_gather_shares", "gq_lnq", "gq_lnq_workspace_bytes",
+    "gq_token_logprobs", "gq_token_logprobs_grad",
 )
 GQ_HESSIAN_DETERMINISTIC = 1      # flag of gq_hessian_accumulate: single writer per element of H
 GQ_HESSIAN_S_PREPARED = 2         # flag of gq_hessian_accumulate: the workspace was filled by gq_saliency_prepared
 KERNEL_NAMES = ("saliency", "hessian", "mirror", "split_delta", "gram_dot", "reduce", "split_saliency", "cd_panel",
-                "cd_block", "cd_aux", "cb_gemm", "cb_fold", "cb_aux", "exchange")
+                "cd_block", "cd_aux", "cb_gemm", "cb_fold", "cb_aux", "exchange", "score")
 
 
 class GQError(RuntimeError):
@@ -101,6 +102,10 @@ def lib() -> ctypes.CDLL:
         L.gq_lnq_workspace_bytes.argtypes = [i64, i64, i32, i32]
         L.gq_lnq.restype = i32
         L.gq_lnq.argtypes = [vp, vp, i32, i64, i64, vp, i32, i32, i32, ctypes.c_double, vp, vp, vp, sz, vp]
+        L.gq_token_logprobs.restype = i32
+        L.gq_token_logprobs.argtypes = [vp, i32, i64, i64, i64, vp, i32, vp, vp, vp, vp, vp, vp]
+        L.gq_token_logprobs_grad.restype = i32
+        L.gq_token_logprobs_grad.argtypes = [vp, i32, i64, i64, i64, vp, vp, vp, vp, vp, vp, i64, vp]
         L.gq_selftest_wait_timeout.restype = i32
         L.gq_selftest_wait_timeout.argtypes = [i32, vp]
         L.gq_kernel_timing_enable.restype = i32
@@ -616,3 +621,68 @@ def gq_codebook_update(W: torch.Tensor, Q: torch.Tensor, m: int, H: torch.Tensor
     if rc:
         raise GQError("gq_codebook_update", rc)
     return codebook, W_hat
+
+
+def _logits(t: torch.Tensor, name: str):
+    """(dtype code, n, vocab, leading dimension) of a CUDA tensor of logits."""
+    if not t.is_cuda or t.dtype not in _DTYPE_CODES:
+        raise ValueError("%s must be a CUDA tensor of dtype bfloat16, float16 or float32" % name)
+    return (_DTYPE_CODES[t.dtype],) + _rows(t, name)
+
+
+def _vector(t: Optional[torch.Tensor], n: int, dtype, name: str, width: int = 0) -> int:
+    """Pointer of a contiguous [n] (or [n, width]) tensor, 0 for None."""
+    if t is None:
+        return 0
+    _dev(t, dtype, name)
+    if tuple(t.shape) != ((n, width) if width else (n,)) or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s tensor" % (name, "[%d, %d]" % (n, width) if width else "[%d]" % n))
+    return t.data_ptr()
+
+
+def gq_token_logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor] = None, top: int = 0, stream=None):
+    """Log probabilities of the ``targets`` (int64 ``[n]``; outside ``[0, vocab)``: not counted, 0), entropies, softmax
+    statistics and the ``top`` highest log probabilities with their indices, for every row of ``logits`` (``[n, vocab]``).
+    Returns ``(logp [n], entropy [n], stats [n, 2], top_logp [n, top], top_ids [n, top])``, the first ``None`` without
+    targets, the last two without alternatives."""
+    code, n, vocab, ld = _logits(logits, "logits")
+    top = int(top)
+    t_ptr = _vector(targets, n, torch.int64, "targets")
+    dev = logits.device
+    rows = torch.empty((4, n), dtype=torch.float32, device=dev)
+    entropy, stats = rows[1], rows[2:].view(-1).view(n, 2)
+    logp = rows[0] if targets is not None else None
+    top_logp = top_ids = None
+    if top > 0:
+        top_logp = torch.empty((n, top), dtype=torch.float32, device=dev)
+        top_ids = torch.empty((n, top), dtype=torch.int32, device=dev)
+    tensors = (logits,) if targets is None else (logits, targets)
+    _call("gq_token_logprobs",
+          (logits.data_ptr(), code, n, vocab, ld, t_ptr, top, logp.data_ptr() if logp is not None else 0, entropy.data_ptr(),
+           stats.data_ptr(), top_logp.data_ptr() if top > 0 else 0, top_ids.data_ptr() if top > 0 else 0),
+          stream, ("logits", "targets"), tensors)
+    return logp, entropy, stats, top_logp, top_ids
+
+
+def gq_token_logprobs_grad(logits: torch.Tensor, targets: Optional[torch.Tensor], stats: torch.Tensor, entropy: Optional[torch.Tensor] = None,
+                           d_logp: Optional[torch.Tensor] = None, d_entropy: Optional[torch.Tensor] = None,
+                           d_logits: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Gradient in the logits of ``sum(d_logp * logp) + sum(d_entropy * entropy)``; ``stats`` and ``entropy`` as
+    :func:`gq_token_logprobs` returned them.  The result has the logits' type."""
+    code, n, vocab, ld = _logits(logits, "logits")
+    if d_logits is None:
+        d_logits = torch.empty((n, vocab), dtype=logits.dtype, device=logits.device)
+    _dev(d_logits, logits.dtype, "d_logits")
+    d_n, d_vocab, ld_d = _rows(d_logits, "d_logits")
+    if (d_n, d_vocab) != (n, vocab):
+        raise ValueError("d_logits must have the shape of logits")
+    if d_logp is None:
+        targets = None
+    named = [(k, t) for k, t in (("logits", logits), ("d_logits", d_logits), ("targets", targets), ("stats", stats), ("entropy", entropy),
+                                 ("d_logp", d_logp), ("d_entropy", d_entropy)) if t is not None]
+    _call("gq_token_logprobs_grad",
+          (logits.data_ptr(), code, n, vocab, ld, _vector(targets, n, torch.int64, "targets"), _vector(stats, n, torch.float32, "stats", 2),
+           _vector(entropy, n, torch.float32, "entropy"), _vector(d_logp, n, torch.float32, "d_logp"),
+           _vector(d_entropy, n, torch.float32, "d_entropy"), d_logits.data_ptr(), ld_d),
+          stream, tuple(k for k, _ in named), tuple(t for _, t in named))
+    return d_logits

@@ -21,6 +21,7 @@
 #include "gq_codebook_gemm.cuh"
 #include "gq_gram_dot.cuh"
 #include "gq_kernels.cuh"
+#include "gq_score.cuh"
 
 #define GQ_VERSION_NUMBER 100   /* 0.1.0 */
 
@@ -83,6 +84,27 @@ template <typename... Params, typename... Args>
 void launch(void (*kernel)(Params...), dim3 grid, int threads, size_t smem, cudaStream_t st, Args &&...args)
 {
     launch_as(true, kernel, grid, threads, smem, st, static_cast<Args &&>(args)...);
+}
+
+// launch() with clusters of `ranks` consecutive blocks.
+template <typename... Params, typename... Args>
+void launch_cluster(void (*kernel)(Params...), unsigned ranks, dim3 grid, int threads, size_t smem, cudaStream_t st, Args &&...args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(static_cast<unsigned>(threads));
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = ranks;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    (void)cudaLaunchKernelEx(&cfg, kernel, static_cast<Params>(args)...);
 }
 
 // Per-device status word {status, site, block, unit}; written by kernels, read by gq_check().
@@ -1277,6 +1299,112 @@ int32_t gq_lnq(const float *W, uint8_t *Q, int32_t m, int64_t d_in, int64_t d_ou
         if (int32_t rc = cd_cycles_impl(W, W_hat, Q, codebook, m, d_in, d_out, H, g, K, workspace, Lc, st)) return rc;
     }
     return codebook_update_impl(W, Q, m, d_in, d_out, g, lambda, codebook, W_hat, workspace, Lb, st);
+}
+
+// Elements of a gq_dtype in bytes, 0 for anything else.
+static size_t dtype_bytes(int32_t dtype)
+{
+    return dtype == GQ_DTYPE_FP32 ? 4 : (dtype == GQ_DTYPE_BF16 || dtype == GQ_DTYPE_FP16) ? 2 : 0;
+}
+
+static int32_t check_logits_shape(int32_t dtype, int64_t n, int64_t vocab, int64_t ld)
+{
+    if (dtype_bytes(dtype) == 0 || n < 0 || vocab < 1 || ld < vocab) return GQ_ERR_INVALID_ARG;
+    if (vocab > (1ll << 30) || n >= (1ll << 28) || ld > (1ll << 40)) return GQ_ERR_UNSUPPORTED_SHAPE;
+    return GQ_OK;
+}
+
+int32_t gq_token_logprobs(const void *logits, int32_t dtype, int64_t n, int64_t vocab, int64_t ld, const int64_t *targets,
+                          int32_t top, float *logp, float *entropy, float *stats, float *top_logp, int32_t *top_ids,
+                          void *stream)
+{
+    if (int32_t rc = check_logits_shape(dtype, n, vocab, ld)) return rc;
+    if (top < 0 || top > vocab) return GQ_ERR_INVALID_ARG;
+    if (top > gq::SC_MAX_TOP) return GQ_ERR_UNSUPPORTED_SHAPE;
+    if (n == 0) return GQ_OK;
+    if (!logits || !entropy || !stats || (targets == nullptr) != (logp == nullptr) || (top > 0 && (!top_logp || !top_ids)))
+        return GQ_ERR_INVALID_ARG;
+    if (!aligned(logits, dtype_bytes(dtype)) || (targets && !aligned(targets, 8)) || (logp && !aligned(logp, 4)) || !aligned(entropy, 4) ||
+        !aligned(stats, 4) || (top > 0 && (!aligned(top_logp, 4) || !aligned(top_ids, 4))))
+        return GQ_ERR_ALIGNMENT;
+    const size_t rows = static_cast<size_t>(n), alt = top > 0 ? rows * top * 4 : 0;
+    const ByteRange wr[5] = {{logp, rows * 4}, {entropy, rows * 4}, {stats, rows * 8}, {top_logp, alt}, {top_ids, alt}};
+    const ByteRange ro[2] = {{logits, span_bytes(n, vocab, ld, dtype_bytes(dtype))}, {targets, rows * 8}};
+    if (int32_t rc = check_disjoint(wr, ro)) return rc;
+    DeviceInfo *di;
+    if (int32_t rc = device_info(&di)) return rc;
+    // Rows are split while there are fewer CTAs than SMs and a CTA keeps a round of 16-byte loads.
+    unsigned ranks = 1;
+    const int64_t chunks = vocab * static_cast<int64_t>(dtype_bytes(dtype)) / 16;
+    while (ranks < gq::SC_MAX_CLUSTER && n * ranks < di->sm_count && chunks >= 2 * ranks * gq::SC_THREADS) ranks *= 2;
+    gq::ScoreParams p{};
+    p.logits = logits;
+    p.ld = ld;
+    p.vocab = static_cast<int>(vocab);
+    p.top = top;
+    p.targets = reinterpret_cast<const long long *>(targets);
+    p.logp = logp;
+    p.entropy = entropy;
+    p.stats = stats;
+    p.top_logp = top_logp;
+    p.top_ids = top_ids;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    {
+        LaunchScope scope(GQ_KERNEL_SCORE, st);
+        const auto kernel = dtype == GQ_DTYPE_BF16 ? gq::token_logprobs_kernel<0> : dtype == GQ_DTYPE_FP16 ? gq::token_logprobs_kernel<1>
+                                                                                                      : gq::token_logprobs_kernel<2>;
+        launch_cluster(kernel, ranks, dim3(static_cast<unsigned>(n) * ranks), gq::SC_THREADS, 0, st, p, static_cast<int>(ranks));
+    }
+    GQ_CUDA(cudaGetLastError());
+    return GQ_OK;
+}
+
+int32_t gq_token_logprobs_grad(const void *logits, int32_t dtype, int64_t n, int64_t vocab, int64_t ld, const int64_t *targets,
+                               const float *stats, const float *entropy, const float *d_logp, const float *d_entropy,
+                               void *d_logits, int64_t ld_d, void *stream)
+{
+    if (int32_t rc = check_logits_shape(dtype, n, vocab, ld)) return rc;
+    if (ld_d < vocab) return GQ_ERR_INVALID_ARG;
+    if (ld_d > (1ll << 40)) return GQ_ERR_UNSUPPORTED_SHAPE;
+    if (n == 0) return GQ_OK;
+    const size_t elem = dtype_bytes(dtype);
+    if (!logits || !stats || !d_logits || (targets == nullptr) != (d_logp == nullptr) || (!d_logp && !d_entropy) || (d_entropy && !entropy))
+        return GQ_ERR_INVALID_ARG;
+    if (!aligned(logits, elem) || !aligned(d_logits, elem) || !aligned(stats, 4) || (targets && !aligned(targets, 8)) ||
+        (d_logp && !aligned(d_logp, 4)) || (d_entropy && (!aligned(d_entropy, 4) || !aligned(entropy, 4))))
+        return GQ_ERR_ALIGNMENT;
+    const size_t rows = static_cast<size_t>(n);
+    const ByteRange wr[1] = {{d_logits, span_bytes(n, vocab, ld_d, elem)}};
+    const ByteRange ro[6] = {{logits, span_bytes(n, vocab, ld, elem)}, {targets, rows * 8}, {stats, rows * 8}, {entropy, rows * 4},
+                             {d_logp, rows * 4}, {d_entropy, rows * 4}};
+    if (int32_t rc = check_disjoint(wr, ro)) return rc;
+    const int64_t per = static_cast<int64_t>(16 / elem) * gq::SC_GRAD_THREADS * gq::SC_GRAD_CHUNKS;
+    const int64_t parts = (vocab + per - 1) / per;
+    if (n * parts >= (1ll << 31)) return GQ_ERR_UNSUPPORTED_SHAPE;
+    DeviceInfo *di;
+    if (int32_t rc = device_info(&di)) return rc;
+    gq::ScoreGradParams p{};
+    p.logits = logits;
+    p.ld = ld;
+    p.vocab = static_cast<int>(vocab);
+    p.targets = reinterpret_cast<const long long *>(targets);
+    p.stats = stats;
+    p.entropy = entropy;
+    p.d_logp = d_logp;
+    p.d_entropy = d_entropy;
+    p.d_logits = d_logits;
+    p.ld_d = ld_d;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    {
+        LaunchScope scope(GQ_KERNEL_SCORE, st);
+        const bool ent = d_entropy != nullptr;
+        const auto kernel = dtype == GQ_DTYPE_BF16 ? (ent ? gq::token_logprobs_grad_kernel<0, true> : gq::token_logprobs_grad_kernel<0, false>)
+                          : dtype == GQ_DTYPE_FP16 ? (ent ? gq::token_logprobs_grad_kernel<1, true> : gq::token_logprobs_grad_kernel<1, false>)
+                                                   : (ent ? gq::token_logprobs_grad_kernel<2, true> : gq::token_logprobs_grad_kernel<2, false>);
+        launch(kernel, dim3(static_cast<unsigned>(n * parts)), gq::SC_GRAD_THREADS, 0, st, p, static_cast<int>(parts));
+    }
+    GQ_CUDA(cudaGetLastError());
+    return GQ_OK;
 }
 
 int32_t gq_selftest_wait_timeout(int32_t budget_ms, void *stream)
