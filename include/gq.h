@@ -366,6 +366,63 @@ int32_t gq_token_logprobs_grad(const void *logits, int32_t dtype, int64_t n, int
                                void *d_logits, int64_t ld_d, void *stream);
 
 /*
+ * Products with a quantised layer, from the codes and levels that gq_lnq leaves (the layer's forward pass, of which the capture of
+ * activations and the evaluation of a quantised model consist).
+ *
+ * gq_linear_pack lays the weights out once: `codes` = two codes a byte, the lower four bits first, rows of 16 ceil(d_in / 32) bytes
+ * (zero behind d_in; gq_linear_codes_bytes in all), `table` = [d_out, 16] levels rounded to `dtype`, zero from m on.
+ *
+ *   Q          uint8 [d_out, d_in], codes < m (larger ones are taken as m - 1); codebook fp32 [d_out, m], 1 <= m <= 16
+ *   dtype      GQ_DTYPE_BF16 or GQ_DTYPE_FP16: the type of the activations the layer will see
+ *   codes, table     16-byte aligned
+ * Shapes of this and the following calls: d_in % 8 == 0, d_out % 8 == 0, both at most 2^20.
+ */
+int32_t gq_linear_pack(const uint8_t *Q, const float *codebook, int32_t m, int64_t d_in, int64_t d_out, int32_t dtype,
+                       uint8_t *codes, void *table, void *stream);
+size_t gq_linear_codes_bytes(int64_t d_in, int64_t d_out);
+
+/*
+ * One layer forward, with bias, activation and residual:
+ *     z_ij = sum_c X[i][c] table[j][code[j][c]] + bias[j],     Y[i][j] = act(z_ij) + residual[i][j]
+ *
+ *   X          [n, ld_x] of `dtype`, 16-byte aligned, ld_x >= d_in, ld_x % 8 == 0; 0 <= n <= 2^28 (0 is a no-op)
+ *   m          as given to gq_linear_pack (up to 8 levels are looked up faster)
+ *   bias       [d_out] of `dtype` or NULL; residual [n, ld_r] of `dtype` (rules as for X) or NULL
+ *   activation enum gq_activation; GELU is the exact one (error function)
+ *   Y          [n, ld_y] of `dtype` (rules as for X)
+ *   Z          [n, ld_z] of `dtype` or NULL: the pre-activation, rounded, for gq_linear_grad
+ * Sums are fp32, everything behind them too, rounded once at the end.  Levels are finite; what stands behind d_in in codes and X is
+ * not looked at.  One launch: up to 8 tokens on kernels that read the codes once at memory speed, more on tensor cores.
+ * Results are bit-reproducible.
+ */
+enum gq_activation { GQ_ACT_NONE = 0, GQ_ACT_RELU = 1, GQ_ACT_SILU = 2, GQ_ACT_GELU = 3 };
+int32_t gq_linear(const void *X, int32_t dtype, int64_t n, int64_t d_in, int64_t ld_x, const uint8_t *codes, const void *table,
+                  int32_t m, int64_t d_out, const void *bias, int32_t activation, const void *residual, int64_t ld_r, void *Y,
+                  int64_t ld_y, void *Z, int64_t ld_z, void *stream);
+
+/*
+ * Its backward pass:
+ *     dZ = dY act'(Z), rounded to `dtype` (this is the dl/dZ that gq_saliency reduces), and from the rounded dZ
+ *     dX[i][c] = sum_j dZ[i][j] table[j][code[j][c]]
+ *     d_table[j][l] = sum over the c with code[j][c] = l of sum_i dZ[i][j] X[i][c]
+ *     d_bias[j] = sum_i dZ[i][j]                         (the residual's gradient is dY itself)
+ *
+ *   dY         [n, ld_dy] of `dtype`; Z [n, ld_z] as left by gq_linear and dZ [n, ld_dz], out: both with an activation, both NULL
+ *              without one (dY is dZ then)
+ *   X          as given to gq_linear; NULL where d_table is not asked for
+ *   dX         [n, ld_dx] of `dtype` or NULL; d_table fp32 [d_out, m] or NULL; d_bias fp32 [d_out] or NULL
+ *   workspace  at least gq_linear_grad_workspace_bytes(n, d_in, d_out) bytes, 1024-byte aligned; NULL where neither d_table nor d_bias
+ *              is asked for
+ * All matrices by the rules of gq_linear's X.  d_table and d_bias are overwritten (zero for n = 0).  Sums are fp32 on the tensor cores over
+ * at most 1024 tokens at a time for d_table, partial sums are added in a fixed order: results are bit-reproducible.
+ */
+int32_t gq_linear_grad(const void *dY, int32_t dtype, int64_t n, int64_t d_out, int64_t ld_dy, const void *Z, int64_t ld_z,
+                       int32_t activation, const void *X, int64_t d_in, int64_t ld_x, const uint8_t *codes, const void *table, int32_t m,
+                       void *dZ, int64_t ld_dz, void *dX, int64_t ld_dx, float *d_table, float *d_bias, void *workspace,
+                       size_t workspace_bytes, void *stream);
+size_t gq_linear_grad_workspace_bytes(int64_t n, int64_t d_in, int64_t d_out);
+
+/*
  * Synchronises `stream`, then returns and clears the first device-side error recorded on the
  * current device since the last gq_check (GQ_OK if none).  A pipeline wait inside a kernel that
  * exceeds its time budget (2 s by default; environment variable GQ_WAIT_BUDGET_MS) makes the
@@ -454,7 +511,9 @@ enum gq_kernel_id {
     GQ_KERNEL_CB_AUX = 12,     /* codebook step: splits, transposes, one-hot columns, W_hat */
     GQ_KERNEL_EXCHANGE = 13,   /* token-sharded accumulation: reduce / gather of blocks of H over peer memory */
     GQ_KERNEL_SCORE = 14,      /* log probabilities of tokens and their gradient         */
-    GQ_KERNEL_COUNT = 15
+    GQ_KERNEL_LINEAR = 15,     /* products with quantised weights, gradient of the levels */
+    GQ_KERNEL_LINEAR_AUX = 16, /* layout of codes, activation gradient, sums of partial results */
+    GQ_KERNEL_COUNT = 17
 };
 
 /*

@@ -27,11 +27,13 @@ EXPORTS = (
     "gq_selftest_wait_timeout", "gq_codebook_update", "gq_codebook_workspace_bytes",
     "gq_hessian_reduce_share", "gq_hessian_gather_shares", "gq_lnq", "gq_lnq_workspace_bytes",
     "gq_token_logprobs", "gq_token_logprobs_grad",
+    "gq_linear_pack", "gq_linear_codes_bytes", "gq_linear", "gq_linear_grad", "gq_linear_grad_workspace_bytes",
 )
 GQ_HESSIAN_DETERMINISTIC = 1      # flag of gq_hessian_accumulate: single writer per element of H
 GQ_HESSIAN_S_PREPARED = 2         # flag of gq_hessian_accumulate: the workspace was filled by gq_saliency_prepared
+GQ_ACT_NONE, GQ_ACT_RELU, GQ_ACT_SILU, GQ_ACT_GELU = 0, 1, 2, 3      # activations of gq_linear
 KERNEL_NAMES = ("saliency", "hessian", "mirror", "split_delta", "gram_dot", "reduce", "split_saliency", "cd_panel",
-                "cd_block", "cd_aux", "cb_gemm", "cb_fold", "cb_aux", "exchange", "score")
+                "cd_block", "cd_aux", "cb_gemm", "cb_fold", "cb_aux", "exchange", "score", "linear", "linear_aux")
 
 
 class GQError(RuntimeError):
@@ -106,6 +108,16 @@ def lib() -> ctypes.CDLL:
         L.gq_token_logprobs.argtypes = [vp, i32, i64, i64, i64, vp, i32, vp, vp, vp, vp, vp, vp]
         L.gq_token_logprobs_grad.restype = i32
         L.gq_token_logprobs_grad.argtypes = [vp, i32, i64, i64, i64, vp, vp, vp, vp, vp, vp, i64, vp]
+        L.gq_linear_codes_bytes.restype = sz
+        L.gq_linear_codes_bytes.argtypes = [i64, i64]
+        L.gq_linear_pack.restype = i32
+        L.gq_linear_pack.argtypes = [vp, vp, i32, i64, i64, i32, vp, vp, vp]
+        L.gq_linear.restype = i32
+        L.gq_linear.argtypes = [vp, i32, i64, i64, i64, vp, vp, i32, i64, vp, i32, vp, i64, vp, i64, vp, i64, vp]
+        L.gq_linear_grad_workspace_bytes.restype = sz
+        L.gq_linear_grad_workspace_bytes.argtypes = [i64, i64, i64]
+        L.gq_linear_grad.restype = i32
+        L.gq_linear_grad.argtypes = [vp, i32, i64, i64, i64, vp, i64, i32, vp, i64, i64, vp, vp, i32, vp, i64, vp, i64, vp, vp, vp, sz, vp]
         L.gq_selftest_wait_timeout.restype = i32
         L.gq_selftest_wait_timeout.argtypes = [i32, vp]
         L.gq_kernel_timing_enable.restype = i32
@@ -686,3 +698,110 @@ def gq_token_logprobs_grad(logits: torch.Tensor, targets: Optional[torch.Tensor]
            _vector(d_entropy, n, torch.float32, "d_entropy"), d_logits.data_ptr(), ld_d),
           stream, tuple(k for k, _ in named), tuple(t for _, t in named))
     return d_logits
+
+
+def gq_linear_codes_bytes(d_in: int, d_out: int) -> int:
+    return int(lib().gq_linear_codes_bytes(d_in, d_out))
+
+
+def gq_linear_pack(Q: torch.Tensor, codebook: torch.Tensor, dtype=torch.bfloat16, stream=None):
+    """The layout :func:`gq_linear` reads: ``(codes, table)`` from the quantiser's ``Q`` (uint8 ``[d_out, d_in]``) and ``codebook``
+    (fp32 ``[d_out, m]``) for activations of ``dtype`` (bfloat16 or float16)."""
+    _dev(Q, torch.uint8, "Q")
+    _dev(codebook, torch.float32, "codebook")
+    if dtype not in (torch.bfloat16, torch.float16):
+        raise ValueError("dtype must be bfloat16 or float16")
+    if Q.dim() != 2 or not Q.is_contiguous():
+        raise ValueError("Q must be contiguous [d_out, d_in]")
+    d_out, d_in = Q.shape
+    if codebook.dim() != 2 or codebook.shape[0] != d_out or not codebook.is_contiguous():
+        raise ValueError("codebook must be a contiguous [d_out, m] tensor")
+    codes = torch.empty((d_out, (d_in + 31) // 32 * 16), dtype=torch.uint8, device=Q.device)
+    table = torch.empty((d_out, 16), dtype=dtype, device=Q.device)
+    _call("gq_linear_pack", (Q.data_ptr(), codebook.data_ptr(), codebook.shape[1], d_in, d_out, _DTYPE_CODES[dtype], codes.data_ptr(),
+                             table.data_ptr()), stream, ("Q", "codebook"), (Q, codebook))
+    return codes, table
+
+
+def _linear_weights(X: torch.Tensor, codes: torch.Tensor, table: torch.Tensor, d_in: int) -> int:
+    """d_out of packed weights; ValueError unless they fit activations like X of width d_in."""
+    if not X.is_cuda or X.dtype not in (torch.bfloat16, torch.float16):
+        raise ValueError("activations must be CUDA tensors of dtype bfloat16 or float16")
+    _dev(codes, torch.uint8, "codes")
+    _dev(table, X.dtype, "table")
+    d_out = codes.shape[0]
+    if codes.dim() != 2 or codes.shape[1] != (d_in + 31) // 32 * 16 or not codes.is_contiguous():
+        raise ValueError("codes must be contiguous [d_out, 16 * ceil(d_in / 32)] as gq_linear_pack leaves them")
+    if tuple(table.shape) != (d_out, 16) or not table.is_contiguous():
+        raise ValueError("table must be a contiguous [d_out, 16] tensor")
+    return d_out
+
+
+def _matrix(t: Optional[torch.Tensor], shape, dtype, name: str):
+    """(pointer, leading dimension) of a matrix with a contiguous last dimension, (0, 0) for None."""
+    if t is None:
+        return 0, 0
+    _dev(t, dtype, name)
+    rows, width, ld = _rows(t, name)
+    if (rows, width) != shape:
+        raise ValueError("%s must be %s" % (name, list(shape)))
+    return t.data_ptr(), ld
+
+
+def gq_linear(X: torch.Tensor, codes: torch.Tensor, table: torch.Tensor, m: int, bias: Optional[torch.Tensor] = None,
+              activation: int = GQ_ACT_NONE, residual: Optional[torch.Tensor] = None, Y: Optional[torch.Tensor] = None,
+              Z: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """``activation(X W_hat^T + bias) + residual`` with ``W_hat[j, c] = table[j, code[j, c]]`` (:func:`gq_linear_pack`).  Returns
+    ``Y`` ``[n, d_out]`` in the type of ``X``; ``Z``, if given, receives the pre-activation for :func:`gq_linear_grad`."""
+    n, d_in, ld_x = _rows(X, "X")
+    d_out = _linear_weights(X, codes, table, d_in)
+    if Y is None:
+        Y = torch.empty((n, d_out), dtype=X.dtype, device=X.device)
+    y_ptr, ld_y = _matrix(Y, (n, d_out), X.dtype, "Y")
+    z_ptr, ld_z = _matrix(Z, (n, d_out), X.dtype, "Z")
+    r_ptr, ld_r = _matrix(residual, (n, d_out), X.dtype, "residual")
+    names, tensors = ("X", "codes", "table", "Y"), (X, codes, table, Y)
+    if bias is not None or residual is not None or Z is not None:
+        extra = [(k, t) for k, t in (("bias", bias), ("residual", residual), ("Z", Z)) if t is not None]
+        names, tensors = names + tuple(k for k, _ in extra), tensors + tuple(t for _, t in extra)
+    _call("gq_linear",
+          (X.data_ptr(), _DTYPE_CODES[X.dtype], n, d_in, ld_x, codes.data_ptr(), table.data_ptr(), int(m), d_out,
+           _vector(bias, d_out, X.dtype, "bias"), int(activation), r_ptr, ld_r, y_ptr, ld_y, z_ptr, ld_z), stream, names, tensors)
+    return Y
+
+
+def gq_linear_grad_workspace_bytes(n: int, d_in: int, d_out: int) -> int:
+    return int(lib().gq_linear_grad_workspace_bytes(n, d_in, d_out))
+
+
+def gq_linear_grad(dY: torch.Tensor, X: torch.Tensor, codes: torch.Tensor, table: torch.Tensor, m: int, workspace: Optional[torch.Tensor] = None,
+                   Z: Optional[torch.Tensor] = None, activation: int = GQ_ACT_NONE, need_x: bool = True, need_table: bool = True,
+                   need_bias: bool = True, dZ: Optional[torch.Tensor] = None, dX: Optional[torch.Tensor] = None, stream=None):
+    """Backward pass of :func:`gq_linear`: ``(dZ, dX, d_table, d_bias)``.  ``dZ`` (the gradient of the pre-activation, what
+    :func:`gq_saliency` reduces) is ``dY`` itself without an activation; ``d_table`` (fp32 ``[d_out, m]``) and ``d_bias`` (fp32 ``[d_out]``)
+    need the workspace.  What is not needed comes back as ``None``."""
+    n, d_in, ld_x = _rows(X, "X")
+    d_out = _linear_weights(X, codes, table, d_in)
+    dy_ptr, ld_dy = _matrix(dY, (n, d_out), X.dtype, "dY")
+    z_ptr, ld_z = _matrix(Z, (n, d_out), X.dtype, "Z")
+    m = int(m)
+    if activation == GQ_ACT_NONE:
+        if dZ is not None:
+            raise ValueError("dZ is dY without an activation")
+    elif dZ is None:
+        dZ = torch.empty((n, d_out), dtype=X.dtype, device=X.device)
+    if dX is None and need_x:
+        dX = torch.empty((n, d_in), dtype=X.dtype, device=X.device)
+    dz_ptr, ld_dz = _matrix(dZ, (n, d_out), X.dtype, "dZ")
+    dx_ptr, ld_dx = _matrix(dX, (n, d_in), X.dtype, "dX")
+    d_table = torch.empty((d_out, max(m, 1)), dtype=torch.float32, device=X.device) if need_table else None
+    d_bias = torch.empty((d_out,), dtype=torch.float32, device=X.device) if need_bias else None
+    named = [(k, t) for k, t in (("dY", dY), ("X", X), ("codes", codes), ("table", table), ("Z", Z), ("dZ", dZ), ("dX", dX),
+                                 ("workspace", workspace)) if t is not None]
+    _call("gq_linear_grad",
+          (dy_ptr, _DTYPE_CODES[X.dtype], n, d_out, ld_dy, z_ptr, ld_z, int(activation), X.data_ptr(), d_in, ld_x, codes.data_ptr(),
+           table.data_ptr(), m, dz_ptr, ld_dz, dx_ptr, ld_dx, d_table.data_ptr() if need_table else 0, d_bias.data_ptr() if need_bias else 0,
+           workspace.data_ptr() if workspace is not None else 0,
+           workspace.numel() * workspace.element_size() if workspace is not None else 0),
+          stream, tuple(k for k, _ in named), tuple(t for _, t in named))
+    return (dY if activation == GQ_ACT_NONE else dZ), dX, d_table, d_bias

@@ -21,6 +21,7 @@
 #include "gq_codebook_gemm.cuh"
 #include "gq_gram_dot.cuh"
 #include "gq_kernels.cuh"
+#include "gq_linear.cuh"
 #include "gq_score.cuh"
 
 #define GQ_VERSION_NUMBER 100   /* 0.1.0 */
@@ -191,6 +192,11 @@ int32_t device_info(DeviceInfo **out)
         GQ_CUDA(cudaFuncSetAttribute(gq::cd_block_kernel<8, 16>, cudaFuncAttributeMaxDynamicSharedMemorySize, gq::cd_smem_bytes(16)));
         GQ_CUDA(cudaFuncSetAttribute(gq::cd_block_kernel<16, 32>, cudaFuncAttributeMaxDynamicSharedMemorySize, gq::cd_smem_bytes(32)));
         GQ_CUDA(cudaFuncSetAttribute(gq::cd_block_kernel<16, 16>, cudaFuncAttributeMaxDynamicSharedMemorySize, gq::cd_smem_bytes(16)));
+        GQ_CUDA(cudaFuncSetAttribute(gq::linear_pair_kernel<false, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, gq::LP_SMEM_BYTES));
+        GQ_CUDA(cudaFuncSetAttribute(gq::linear_pair_kernel<false, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, gq::LP_SMEM_BYTES));
+        GQ_CUDA(cudaFuncSetAttribute(gq::linear_pair_kernel<true, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, gq::LP_SMEM_BYTES));
+        GQ_CUDA(cudaFuncSetAttribute(gq::linear_pair_kernel<true, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, gq::LP_SMEM_BYTES));
+        GQ_CUDA(cudaFuncSetAttribute(gq::linear_level_grad_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, gq::LG_SMEM_BYTES));
         GQ_CUDA(cudaFuncSetAttribute(gq::hessian_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                      gq::HS_SMEM_BYTES));
         {
@@ -1402,6 +1408,294 @@ int32_t gq_token_logprobs_grad(const void *logits, int32_t dtype, int64_t n, int
                           : dtype == GQ_DTYPE_FP16 ? (ent ? gq::token_logprobs_grad_kernel<1, true> : gq::token_logprobs_grad_kernel<1, false>)
                                                    : (ent ? gq::token_logprobs_grad_kernel<2, true> : gq::token_logprobs_grad_kernel<2, false>);
         launch(kernel, dim3(static_cast<unsigned>(n * parts)), gq::SC_GRAD_THREADS, 0, st, p, static_cast<int>(parts));
+    }
+    GQ_CUDA(cudaGetLastError());
+    return GQ_OK;
+}
+
+// ---------------------------------------------------------------- products with quantised weights
+static size_t linear_codes_ld(int64_t d_in) { return static_cast<size_t>((d_in + 31) / 32 * 16); }
+
+static int32_t check_linear_shape(int32_t dtype, int64_t n, int64_t d_in, int64_t d_out, int32_t m)
+{
+    if ((dtype != GQ_DTYPE_BF16 && dtype != GQ_DTYPE_FP16) || n < 0 || d_in < 1 || d_out < 1 || m < 1) return GQ_ERR_INVALID_ARG;
+    if (d_in % 8 != 0 || d_out % 8 != 0 || d_in > (1ll << 20) || d_out > (1ll << 20) || m > gq::LIN_LEVELS || n > (1ll << 28)) return GQ_ERR_UNSUPPORTED_SHAPE;
+    return GQ_OK;
+}
+
+// A 16-bit matrix of n rows: 16-byte rows, leading dimension at least the width.
+static int32_t check_rows16(const void *p, int64_t width, int64_t ld)
+{
+    if (!p || ld < width) return GQ_ERR_INVALID_ARG;
+    if (ld > (1ll << 36)) return GQ_ERR_UNSUPPORTED_SHAPE;
+    return (ld % 8 != 0 || !aligned(p, 16)) ? GQ_ERR_ALIGNMENT : GQ_OK;
+}
+
+size_t gq_linear_codes_bytes(int64_t d_in, int64_t d_out)
+{
+    if (check_linear_shape(GQ_DTYPE_BF16, 0, d_in, d_out, 1) != GQ_OK) return 0;
+    return static_cast<size_t>(d_out) * linear_codes_ld(d_in);
+}
+
+int32_t gq_linear_pack(const uint8_t *Q, const float *codebook, int32_t m, int64_t d_in, int64_t d_out, int32_t dtype, uint8_t *codes, void *table,
+                       void *stream)
+{
+    if (int32_t rc = check_linear_shape(dtype, 0, d_in, d_out, m)) return rc;
+    if (!Q || !codebook || !codes || !table) return GQ_ERR_INVALID_ARG;
+    if (!aligned(codebook, 4) || !aligned(codes, 16) || !aligned(table, 16)) return GQ_ERR_ALIGNMENT;
+    const ByteRange wr[2] = {{codes, gq_linear_codes_bytes(d_in, d_out)}, {table, static_cast<size_t>(d_out) * gq::LIN_LEVELS * 2}};
+    const ByteRange ro[2] = {{Q, static_cast<size_t>(d_out) * d_in}, {codebook, static_cast<size_t>(d_out) * m * 4}};
+    if (int32_t rc = check_disjoint(wr, ro)) return rc;
+    DeviceInfo *di;
+    if (int32_t rc = device_info(&di)) return rc;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    {
+        LaunchScope scope(GQ_KERNEL_LINEAR_AUX, st);
+        launch(gq::linear_pack_kernel, dim3(static_cast<unsigned>(d_out)), 128, 0, st, Q, codebook, m, static_cast<int>(d_in),
+               static_cast<int>(linear_codes_ld(d_in)), dtype == GQ_DTYPE_BF16 ? 1 : 0, codes, static_cast<uint16_t *>(table));
+    }
+    GQ_CUDA(cudaGetLastError());
+    return GQ_OK;
+}
+
+static CUtensorMapDataType map_type(int32_t dtype)
+{
+    return dtype == GQ_DTYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+}
+
+// The tensor-core product: forward (X [n, d_in] -> [n, d_out]) or backward (dZ [n, d_out] -> [n, d_in]).
+static int32_t linear_pair(bool back, gq::LinearParams p, int32_t dtype, const void *in, int64_t ld_in, int32_t m, DeviceInfo *di, cudaStream_t st)
+{
+    const int rows = back ? p.d_in : p.d_out, kdim = back ? p.d_out : p.d_in;
+    const int64_t row_tiles = (rows + gq::TILE_M - 1) / gq::TILE_M, tok_tiles = (p.n + gq::TILE_N - 1) / gq::TILE_N;
+    if (row_tiles * tok_tiles >= (1ll << 30)) return GQ_ERR_UNSUPPORTED_SHAPE;
+    p.row_tiles = static_cast<int>(row_tiles);
+    p.tok_tiles = static_cast<int>(tok_tiles);
+    p.units = static_cast<int>(row_tiles * tok_tiles);
+    p.pairs = p.units < di->max_pairs ? p.units : di->max_pairs;
+    p.status = di->status_ptr;
+    p.wait_budget_ns = wait_budget_ns();
+    CUtensorMap map;
+    if (int32_t rc = make_map(&map, in, kdim, p.n, 1, ld_in, static_cast<int64_t>(p.n) * ld_in, map_type(dtype))) return rc;
+    {
+        LaunchScope scope(GQ_KERNEL_LINEAR, st);
+        const auto kernel = back ? (m > 8 ? gq::linear_pair_kernel<true, true> : gq::linear_pair_kernel<true, false>)
+                                 : (m > 8 ? gq::linear_pair_kernel<false, true> : gq::linear_pair_kernel<false, false>);
+        launch(kernel, dim3(static_cast<unsigned>(2 * p.pairs)), gq::LP_THREADS, gq::LP_SMEM_BYTES, st, map, p);
+    }
+    GQ_CUDA(cudaGetLastError());
+    return GQ_OK;
+}
+
+int32_t gq_linear(const void *X, int32_t dtype, int64_t n, int64_t d_in, int64_t ld_x, const uint8_t *codes, const void *table, int32_t m,
+                  int64_t d_out, const void *bias, int32_t activation, const void *residual, int64_t ld_r, void *Y, int64_t ld_y, void *Z,
+                  int64_t ld_z, void *stream)
+{
+    if (int32_t rc = check_linear_shape(dtype, n, d_in, d_out, m)) return rc;
+    if (activation < GQ_ACT_NONE || activation > GQ_ACT_GELU) return GQ_ERR_INVALID_ARG;
+    if (n == 0) return GQ_OK;
+    if (!codes || !table) return GQ_ERR_INVALID_ARG;
+    if (int32_t rc = check_rows16(X, d_in, ld_x)) return rc;
+    if (int32_t rc = check_rows16(Y, d_out, ld_y)) return rc;
+    if (residual)
+        if (int32_t rc = check_rows16(residual, d_out, ld_r)) return rc;
+    if (Z)
+        if (int32_t rc = check_rows16(Z, d_out, ld_z)) return rc;
+    if (!aligned(codes, 16) || !aligned(table, 16) || (bias && !aligned(bias, 2))) return GQ_ERR_ALIGNMENT;
+    {
+        const ByteRange wr[2] = {{Y, span_bytes(n, d_out, ld_y, 2)}, {Z, span_bytes(n, d_out, ld_z, 2)}};
+        const ByteRange ro[5] = {{X, span_bytes(n, d_in, ld_x, 2)}, {codes, gq_linear_codes_bytes(d_in, d_out)},
+                                 {table, static_cast<size_t>(d_out) * gq::LIN_LEVELS * 2}, {bias, static_cast<size_t>(d_out) * 2},
+                                 {residual, span_bytes(n, d_out, ld_r, 2)}};
+        if (int32_t rc = check_disjoint(wr, ro)) return rc;
+    }
+    DeviceInfo *di;
+    if (int32_t rc = device_info(&di)) return rc;
+    gq::LinearParams p{};
+    p.codes = codes;
+    p.table = static_cast<const uint16_t *>(table);
+    p.ld_codes = static_cast<int>(linear_codes_ld(d_in));
+    p.n = static_cast<int>(n);
+    p.d_in = static_cast<int>(d_in);
+    p.d_out = static_cast<int>(d_out);
+    p.act = activation;
+    p.bf16 = dtype == GQ_DTYPE_BF16 ? 1 : 0;
+    p.bias = static_cast<const uint16_t *>(bias);
+    p.residual = static_cast<const uint16_t *>(residual);
+    p.ld_r = ld_r;
+    p.out = static_cast<uint16_t *>(Y);
+    p.ld_out = ld_y;
+    p.Z = static_cast<uint16_t *>(Z);
+    p.ld_z = ld_z;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (n > gq::LT_TOKENS) return linear_pair(false, p, dtype, X, ld_x, m, di, st);
+    p.X = static_cast<const uint16_t *>(X);
+    p.ld_x = ld_x;
+    // The contraction is split over CTAs while there are fewer of them than SMs and their warps keep a piece each.
+    const unsigned groups = static_cast<unsigned>((d_out + gq::LT_CHANNELS - 1) / gq::LT_CHANNELS);
+    const int64_t pieces = (d_in + gq::LT_K - 1) / gq::LT_K;
+    unsigned ranks = 1;
+    while (ranks < gq::LT_MAX_CLUSTER && groups * ranks < static_cast<unsigned>(di->sm_count) && pieces >= 2 * ranks * gq::LT_WARPS) ranks *= 2;
+    {
+        LaunchScope scope(GQ_KERNEL_LINEAR, st);
+        const auto kernel = p.bf16 ? (m > 8 ? gq::linear_token_kernel<true, true> : gq::linear_token_kernel<true, false>)
+                                   : (m > 8 ? gq::linear_token_kernel<false, true> : gq::linear_token_kernel<false, false>);
+        launch_cluster(kernel, ranks, dim3(groups * ranks), gq::LT_THREADS, 0, st, p, static_cast<int>(ranks));
+    }
+    GQ_CUDA(cudaGetLastError());
+    return GQ_OK;
+}
+
+// Pieces of a channel tile's work in the gradient of the levels: at most this many, so that the scratch does not depend on the device.
+static int64_t level_grad_max_runs(int64_t n, int64_t d_in, int64_t d_out)
+{
+    const int64_t ch_tiles = (d_out + gq::TILE_M - 1) / gq::TILE_M;
+    const int64_t ksteps = (n + gq::TILE_K - 1) / gq::TILE_K;
+    const int64_t units = (d_in + gq::TILE_N - 1) / gq::TILE_N * ((ksteps + gq::LG_CHUNK_KSTEPS - 1) / gq::LG_CHUNK_KSTEPS);
+    int64_t runs = 160 / ch_tiles;
+    if (runs > units) runs = units;
+    return runs < 1 ? 1 : runs;
+}
+
+struct LinearGradLayout {
+    size_t partial, sums, total;
+    int64_t blocks, rows_per_block;
+};
+static LinearGradLayout linear_grad_layout(int64_t n, int64_t d_in, int64_t d_out)
+{
+    LinearGradLayout L;
+    L.rows_per_block = (n + gq::LZ_MAX_BLOCKS - 1) / gq::LZ_MAX_BLOCKS;
+    if (L.rows_per_block < gq::LZ_MIN_ROWS) L.rows_per_block = gq::LZ_MIN_ROWS;
+    L.blocks = (n + L.rows_per_block - 1) / L.rows_per_block;
+    L.partial = 0;
+    L.sums = round_up(static_cast<size_t>(level_grad_max_runs(n, d_in, d_out)) * 2 * d_out * gq::LIN_LEVELS * 4, 1024);
+    L.total = L.sums + round_up(static_cast<size_t>(L.blocks) * d_out * 4, 1024);
+    return L;
+}
+
+size_t gq_linear_grad_workspace_bytes(int64_t n, int64_t d_in, int64_t d_out)
+{
+    if (check_linear_shape(GQ_DTYPE_BF16, n, d_in, d_out, 1) != GQ_OK) return 0;
+    return linear_grad_layout(n, d_in, d_out).total;
+}
+
+int32_t gq_linear_grad(const void *dY, int32_t dtype, int64_t n, int64_t d_out, int64_t ld_dy, const void *Z, int64_t ld_z, int32_t activation,
+                       const void *X, int64_t d_in, int64_t ld_x, const uint8_t *codes, const void *table, int32_t m, void *dZ, int64_t ld_dz,
+                       void *dX, int64_t ld_dx, float *d_table, float *d_bias, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (int32_t rc = check_linear_shape(dtype, n, d_in, d_out, m)) return rc;
+    if (activation < GQ_ACT_NONE || activation > GQ_ACT_GELU) return GQ_ERR_INVALID_ARG;
+    const bool has_act = activation != GQ_ACT_NONE;
+    const size_t table_out = d_table ? static_cast<size_t>(d_out) * m * 4 : 0, bias_out = d_bias ? static_cast<size_t>(d_out) * 4 : 0;
+    if (!aligned(d_table, 4) || !aligned(d_bias, 4)) return GQ_ERR_ALIGNMENT;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (n > 0) {
+        if (has_act != (Z != nullptr) || has_act != (dZ != nullptr) || (!codes && (dX || d_table)) || (!table && dX) || (!X && d_table))
+            return GQ_ERR_INVALID_ARG;
+        if (int32_t rc = check_rows16(dY, d_out, ld_dy)) return rc;
+        if (has_act) {
+            if (int32_t rc = check_rows16(Z, d_out, ld_z)) return rc;
+            if (int32_t rc = check_rows16(dZ, d_out, ld_dz)) return rc;
+        }
+        if (dX)
+            if (int32_t rc = check_rows16(dX, d_in, ld_dx)) return rc;
+        if (d_table)
+            if (int32_t rc = check_rows16(X, d_in, ld_x)) return rc;
+        if (!aligned(codes, 16) || !aligned(table, 16)) return GQ_ERR_ALIGNMENT;
+    }
+    const LinearGradLayout L = linear_grad_layout(n, d_in, d_out);
+    const bool sums = n > 0 && (d_table || d_bias);
+    if (sums) {
+        if (!workspace || workspace_bytes < L.total) return GQ_ERR_WORKSPACE;
+        if (!aligned(workspace, 1024)) return GQ_ERR_ALIGNMENT;
+    }
+    {
+        const ByteRange wr[5] = {{dZ, span_bytes(n, d_out, ld_dz, 2)}, {dX, span_bytes(n, d_in, ld_dx, 2)}, {d_table, table_out}, {d_bias, bias_out},
+                                 {workspace, sums ? L.total : 0}};
+        const ByteRange ro[5] = {{dY, span_bytes(n, d_out, ld_dy, 2)}, {Z, span_bytes(n, d_out, ld_z, 2)},
+                                 {X, d_table ? span_bytes(n, d_in, ld_x, 2) : 0}, {codes, gq_linear_codes_bytes(d_in, d_out)},
+                                 {table, static_cast<size_t>(d_out) * gq::LIN_LEVELS * 2}};
+        if (int32_t rc = check_disjoint(wr, ro)) return rc;
+    }
+    DeviceInfo *di;
+    if (int32_t rc = device_info(&di)) return rc;
+    if (n == 0) {                                        // sums over no tokens
+        if (d_table) GQ_CUDA(cudaMemsetAsync(d_table, 0, table_out, st));
+        if (d_bias) GQ_CUDA(cudaMemsetAsync(d_bias, 0, bias_out, st));
+        return GQ_OK;
+    }
+    uint8_t *ws = static_cast<uint8_t *>(workspace);
+    float *col_sums = d_bias ? reinterpret_cast<float *>(ws + L.sums) : nullptr;
+    const int bf16 = dtype == GQ_DTYPE_BF16 ? 1 : 0;
+    if (has_act || d_bias) {
+        LaunchScope scope(GQ_KERNEL_LINEAR_AUX, st);
+        launch(gq::linear_dz_kernel, dim3(static_cast<unsigned>((d_out + gq::LZ_COLUMNS - 1) / gq::LZ_COLUMNS), static_cast<unsigned>(L.blocks)),
+               32 * gq::LZ_WARPS, 0, st, static_cast<const uint16_t *>(dY), ld_dy, static_cast<const uint16_t *>(Z), ld_z, activation, bf16,
+               static_cast<int>(n), static_cast<int>(d_out), static_cast<int>(L.rows_per_block), static_cast<uint16_t *>(dZ), ld_dz, col_sums);
+    }
+    GQ_CUDA(cudaGetLastError());
+    const void *grad = has_act ? dZ : dY;
+    const int64_t ld_grad = has_act ? ld_dz : ld_dy;
+    if (dX) {
+        gq::LinearParams p{};
+        p.codes = codes;
+        p.table = static_cast<const uint16_t *>(table);
+        p.ld_codes = static_cast<int>(linear_codes_ld(d_in));
+        p.n = static_cast<int>(n);
+        p.d_in = static_cast<int>(d_in);
+        p.d_out = static_cast<int>(d_out);
+        p.bf16 = bf16;
+        p.out = static_cast<uint16_t *>(dX);
+        p.ld_out = ld_dx;
+        if (int32_t rc = linear_pair(true, p, dtype, grad, ld_grad, m, di, st)) return rc;
+    }
+    int parts = 0;
+    if (d_table) {
+        gq::LevelGradParams p{};
+        p.codes = codes;
+        p.ld_codes = static_cast<int>(linear_codes_ld(d_in));
+        p.n = static_cast<int>(n);
+        p.d_in = static_cast<int>(d_in);
+        p.d_out = static_cast<int>(d_out);
+        p.bf16 = bf16;
+        p.ch_tiles = static_cast<int>((d_out + gq::TILE_M - 1) / gq::TILE_M);
+        p.f_tiles = static_cast<int>((d_in + gq::TILE_N - 1) / gq::TILE_N);
+        const int ksteps = static_cast<int>((n + gq::TILE_K - 1) / gq::TILE_K);
+        p.chunks = (ksteps + gq::LG_CHUNK_KSTEPS - 1) / gq::LG_CHUNK_KSTEPS;
+        p.chunk_ksteps = (ksteps + p.chunks - 1) / p.chunks;
+        p.chunks = (ksteps + p.chunk_ksteps - 1) / p.chunk_ksteps;       // no piece is empty
+        const int64_t units = static_cast<int64_t>(p.f_tiles) * p.chunks;
+        if (units >= (1ll << 30)) return GQ_ERR_UNSUPPORTED_SHAPE;
+        // Runs of a channel tile: as many as make the pair with the most units have the fewest.
+        int64_t most = level_grad_max_runs(n, d_in, d_out), least = INT64_MAX;
+        if (most > units) most = units;
+        for (int64_t r = 1; r <= most; ++r) {
+            const int64_t longest = (p.ch_tiles * r + di->max_pairs - 1) / di->max_pairs * ((units + r - 1) / r);
+            if (longest < least) {
+                least = longest;
+                p.runs = static_cast<int>(r);
+            }
+        }
+        const int64_t items = static_cast<int64_t>(p.ch_tiles) * p.runs;
+        p.pairs = items < di->max_pairs ? static_cast<int>(items) : di->max_pairs;
+        p.partial = reinterpret_cast<float *>(ws + L.partial);
+        p.status = di->status_ptr;
+        p.wait_budget_ns = wait_budget_ns();
+        parts = 2 * p.runs;
+        CUtensorMap mapG, mapX;
+        if (int32_t rc = make_map(&mapG, grad, d_out, n, 1, ld_grad, n * ld_grad, map_type(dtype))) return rc;
+        if (int32_t rc = make_map(&mapX, X, d_in, n, 1, ld_x, n * ld_x, map_type(dtype))) return rc;
+        {
+            LaunchScope scope(GQ_KERNEL_LINEAR, st);
+            launch(gq::linear_level_grad_kernel, dim3(static_cast<unsigned>(2 * p.pairs)), gq::LG_THREADS, gq::LG_SMEM_BYTES, st, mapG, mapX, p);
+        }
+        GQ_CUDA(cudaGetLastError());
+    }
+    if (sums) {
+        LaunchScope scope(GQ_KERNEL_LINEAR_AUX, st);
+        const int64_t threads = d_out * (gq::LIN_LEVELS + 1);
+        launch(gq::linear_sum_kernel, dim3(static_cast<unsigned>((threads + 255) / 256)), 256, 0, st, reinterpret_cast<const float *>(ws + L.partial), parts,
+               static_cast<int>(d_out), m, d_table, reinterpret_cast<const float *>(ws + L.sums), static_cast<int>(L.blocks), d_bias);
     }
     GQ_CUDA(cudaGetLastError());
     return GQ_OK;

@@ -1,0 +1,915 @@
+// Products with weights in the form the quantiser leaves them: a 4-bit code per weight and a table of levels per output channel,
+//
+//   z_ij = sum_c x_ic table[j][code[j][c]] + b_j,    y = act(z) + r
+//   dz = dy act'(z),   dx_ic = sum_j dz_ij table[j][code[j][c]]
+//
+// Layout (linear_pack_kernel): codes [d_out][ld] bytes, two codes a byte, the lower four bits first, ld = 16 ceil(d_in / 32);
+// table [d_out][16] in the activations' type (bf16 or fp16), zero from m on.
+//
+// A level is looked up in registers: a channel's 16 levels are kept as two planes of 16 bytes (low and high bytes, eight
+// registers), and a byte permutation looks four codes up in eight bytes at once.  For four weights: two permutations a plane (levels
+// 0..7 and 8..15), one that takes either by the codes' top bits, and two that join the planes: 2.6 integer instructions a weight, 1.3
+// where m <= 8.  Shared-memory tables would need a load per weight or per pair, with conflicts between the lanes' random codes.
+//
+// Few tokens (linear_token_kernel, n <= 8): bound by the codes' bytes and, behind them, the lookups.  More tokens
+// (linear_pair_kernel): tensor cores, the weight operand written to shared memory by eight lookup warps.
+#pragma once
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "gq_kernels.cuh"
+#include "gq_pipeline.cuh"
+#include "gq_score.cuh"
+
+namespace gq {
+
+constexpr int LIN_LEVELS = 16;
+enum LinearAct { LIN_NONE = 0, LIN_RELU = 1, LIN_SILU = 2, LIN_GELU = 3 };
+
+__device__ __forceinline__ uint4 ld_u32x4(const void *p)
+{
+    uint4 v;
+    asm volatile("ld.global.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
+    return v;
+}
+
+// The levels of a channel as byte planes.
+struct LevelPlanes {
+    uint32_t lo[4], hi[4];
+    __device__ __forceinline__ void set(const uint4 &a, const uint4 &b)
+    {
+        const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            lo[q] = __byte_perm(w[2 * q], w[2 * q + 1], 0x6420);
+            hi[q] = __byte_perm(w[2 * q], w[2 * q + 1], 0x7531);
+        }
+    }
+    // Eight codes -> eight 16-bit levels, in the codes' order.  WIDE: more than eight levels.
+    template <bool WIDE>
+    __device__ __forceinline__ uint4 look(uint32_t q) const
+    {
+        const uint32_t sel = q & 0x77777777u;
+        const uint32_t top = ((q >> 1) & 0x44444444u) | 0x32103210u;
+        uint4 out;
+        uint32_t *o = reinterpret_cast<uint32_t *>(&out);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const uint32_t s = h ? sel >> 16 : sel;
+            uint32_t l = __byte_perm(lo[0], lo[1], s), u = __byte_perm(hi[0], hi[1], s);
+            if (WIDE) {
+                const uint32_t t = h ? top >> 16 : top;
+                l = __byte_perm(l, __byte_perm(lo[2], lo[3], s), t);
+                u = __byte_perm(u, __byte_perm(hi[2], hi[3], s), t);
+            }
+            o[2 * h] = __byte_perm(l, u, 0x5140);
+            o[2 * h + 1] = __byte_perm(l, u, 0x7362);
+        }
+        return out;
+    }
+};
+
+__device__ __forceinline__ float activate(float z, int act)
+{
+    if (act == LIN_RELU) return z > 0.0f ? z : (z != z ? z : 0.0f);
+    if (act == LIN_SILU) return __fdividef(z, 1.0f + __expf(-z));
+    if (act == LIN_GELU) return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
+    return z;
+}
+__device__ __forceinline__ float activation_slope(float z, int act)
+{
+    if (act == LIN_RELU) return z > 0.0f ? 1.0f : 0.0f;
+    if (act == LIN_SILU) {
+        const float sig = __fdividef(1.0f, 1.0f + __expf(-z));
+        return sig * (1.0f + z * (1.0f - sig));
+    }
+    if (act == LIN_GELU) return 0.5f * (1.0f + erff(z * 0.70710678118654752f)) + z * __expf(-0.5f * z * z) * 0.39894228040143268f;
+    return 1.0f;
+}
+
+__device__ __forceinline__ float half_value(uint32_t bits, bool bf16)
+{
+    return bf16 ? __uint_as_float(bits << 16) : __half2float(__ushort_as_half(static_cast<unsigned short>(bits)));
+}
+__device__ __forceinline__ uint32_t half_bits(float v, bool bf16)
+{
+    return bf16 ? __bfloat16_as_ushort(__float2bfloat16_rn(v)) : __half_as_ushort(__float2half_rn(v));
+}
+__device__ __forceinline__ float2 half2_value(uint32_t bits, bool bf16)
+{
+    return bf16 ? make_float2(__uint_as_float(bits << 16), __uint_as_float(bits & 0xffff0000u))
+                : __half22float2(*reinterpret_cast<const __half2 *>(&bits));
+}
+__device__ __forceinline__ uint32_t half2_bits(float x, float y, bool bf16)
+{
+    if (bf16) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
+        return *reinterpret_cast<const uint32_t *>(&h);
+    }
+    const __half2 h = __floats2half2_rn(x, y);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+
+// ------------------------------------------------------------------------------------------------ layout
+// One block per channel: codes as nibbles (larger ones as m - 1, zero behind d_in), levels rounded to the activations' type.
+__global__ void __launch_bounds__(128) linear_pack_kernel(const uint8_t *Q, const float *codebook, int m, int d_in, int ld_codes, int bf16,
+                                                          uint8_t *codes, uint16_t *table)
+{
+    griddep_launch();
+    griddep_wait();
+    const size_t j = blockIdx.x;
+    const uint8_t *q = Q + j * static_cast<size_t>(d_in);
+    uint32_t *out = reinterpret_cast<uint32_t *>(codes + j * static_cast<size_t>(ld_codes));
+    for (int w = threadIdx.x; w < ld_codes / 4; w += 128) {
+        uint32_t v = 0u;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int c = 8 * w + e;
+            if (c < d_in) v |= static_cast<uint32_t>(min(static_cast<int>(q[c]), m - 1)) << (4 * e);
+        }
+        out[w] = v;
+    }
+    if (threadIdx.x < LIN_LEVELS) {
+        const float v = static_cast<int>(threadIdx.x) < m ? codebook[j * m + threadIdx.x] : 0.0f;
+        table[j * LIN_LEVELS + threadIdx.x] = static_cast<uint16_t>(half_bits(v, bf16 != 0));
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ few tokens
+struct LinearParams {
+    const uint8_t *codes;
+    const uint16_t *table;
+    int ld_codes;            // bytes
+    int n, d_in, d_out;
+    int act, bf16;
+    const uint16_t *bias;
+    const uint16_t *residual;
+    long long ld_r;
+    uint16_t *out;           // Y (forward) or dX
+    long long ld_out;
+    uint16_t *Z;
+    long long ld_z;
+    const uint16_t *X;       // few tokens only: the pair kernel reads X through a tensor map
+    long long ld_x;
+    // pair kernel
+    int row_tiles, tok_tiles, units, pairs;
+    uint32_t *status;
+    unsigned long long wait_budget_ns;
+};
+
+constexpr int LT_WARPS = 8;
+constexpr int LT_THREADS = 32 * LT_WARPS;
+constexpr int LT_CHANNELS = 16;
+constexpr int LT_TOKENS = 8;
+constexpr int LT_K = 128;                 // contraction indices a warp takes at a time: 32 per lane of a quad
+constexpr int LT_MAX_CLUSTER = 8;
+
+template <bool BF16>
+__device__ __forceinline__ void mma_m16n8k16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+{
+    if constexpr (BF16)
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                     : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    else
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                     : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// 16 channels per cluster of `ranks` CTAs, the contraction dealt to their warps in pieces of 128.  The order of the contraction indices
+// inside a piece is free as long as both operands share it: lane (g, t) of a quad takes the 32 codes 32 t .. 32 t + 31 of
+// channels g and g + 8 (16 bytes each) and token g's activations at the same place, four codes a product and lane, so that codes
+// are read 64 contiguous bytes a channel and nothing is exchanged between lanes.
+template <bool BF16, bool WIDE>
+__global__ void __launch_bounds__(LT_THREADS) linear_token_kernel(const LinearParams p, int ranks)
+{
+    __shared__ float sums[LT_WARPS][LT_TOKENS][LT_CHANNELS];
+    __shared__ float mine[LT_TOKENS * LT_CHANNELS];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
+    const int group = static_cast<int>(blockIdx.x) / ranks, rank = static_cast<int>(blockIdx.x) - group * ranks;
+    const int j0 = group * LT_CHANNELS;
+    griddep_launch();
+    griddep_wait();
+    // channels are a multiple of 8, so either all of g or all of g + 8 are there
+    const bool second = j0 + 8 < p.d_out;
+    const int ja = j0 + g, jb = second ? ja + 8 : ja;
+    LevelPlanes la, lb;
+    {
+        const uint4 *ta = reinterpret_cast<const uint4 *>(p.table + static_cast<size_t>(ja) * LIN_LEVELS);
+        const uint4 *tb = reinterpret_cast<const uint4 *>(p.table + static_cast<size_t>(jb) * LIN_LEVELS);
+        const uint4 a0 = ld_u32x4(ta), a1 = ld_u32x4(ta + 1), b0 = ld_u32x4(tb), b1 = ld_u32x4(tb + 1);
+        la.set(a0, a1);
+        lb.set(b0, b1);
+    }
+    const uint8_t *ca = p.codes + static_cast<size_t>(ja) * p.ld_codes, *cb = p.codes + static_cast<size_t>(jb) * p.ld_codes;
+    const uint16_t *x = p.X + static_cast<long long>(g < p.n ? g : 0) * p.ld_x;
+    const bool have = g < p.n;
+    float c0[4] = {0.f, 0.f, 0.f, 0.f}, c1[4] = {0.f, 0.f, 0.f, 0.f};
+    const int pieces = (p.d_in + LT_K - 1) / LT_K, stride = ranks * LT_WARPS;
+    struct Piece {
+        uint4 a, b, x[4];
+    };
+    auto fetch = [&](int piece, Piece &f) {
+        const int k = piece * LT_K + 32 * t;
+        const bool in = piece < pieces && k < p.d_in;
+        f.a = in ? ld_once_16(reinterpret_cast<const uint4 *>(ca + (k >> 1))) : make_uint4(0u, 0u, 0u, 0u);
+        f.b = in ? ld_once_16(reinterpret_cast<const uint4 *>(cb + (k >> 1))) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            f.x[q] = (in && have && k + 8 * q < p.d_in) ? ld_u32x4(x + k + 8 * q) : make_uint4(0u, 0u, 0u, 0u);
+    };
+    auto use = [&](int piece, const Piece &f) {
+        const uint32_t qa[4] = {f.a.x, f.a.y, f.a.z, f.a.w}, qb[4] = {f.b.x, f.b.y, f.b.z, f.b.w};
+        const bool ragged = (piece + 1) * LT_K > p.d_in;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            uint4 wa = la.look<WIDE>(qa[q]), wb = lb.look<WIDE>(qb[q]);
+            if (ragged && piece * LT_K + 32 * t + 8 * q >= p.d_in) wa = wb = make_uint4(0u, 0u, 0u, 0u);      // no level meets padding
+            mma_m16n8k16<BF16>(c0, wa.x, wb.x, wa.y, wb.y, f.x[q].x, f.x[q].y);
+            mma_m16n8k16<BF16>(c1, wa.z, wb.z, wa.w, wb.w, f.x[q].z, f.x[q].w);
+        }
+    };
+    int piece = rank * LT_WARPS + warp;
+    Piece cur, next;
+    fetch(piece, cur);
+    for (; piece < pieces; piece += stride) {
+        fetch(piece + stride, next);
+        use(piece, cur);
+        cur = next;
+    }
+    // c[0], c[1]: channel g, tokens 2 t, 2 t + 1; c[2], c[3]: channel g + 8
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sums[warp][2 * t + (e & 1)][g + (e >= 2 ? 8 : 0)] = c0[e] + c1[e];
+    __syncthreads();
+    const int token = tid / LT_CHANNELS, ch = tid % LT_CHANNELS;
+    float z = 0.0f;
+    if (tid < LT_TOKENS * LT_CHANNELS) {
+#pragma unroll
+        for (int w = 0; w < LT_WARPS; ++w) z += sums[w][token][ch];
+        mine[tid] = z;
+    }
+    if (ranks > 1) {
+        cluster_sync_all();
+        if (rank == 0 && tid < LT_TOKENS * LT_CHANNELS) {
+            for (int r = 1; r < ranks; ++r) z += ld_cluster_f32(map_to_cta(smem_u32(&mine[tid]), r));
+        }
+    }
+    const int j = j0 + ch;
+    if (rank == 0 && tid < LT_TOKENS * LT_CHANNELS && token < p.n && j < p.d_out) {
+        if (p.bias) z += half_value(ld_u16(p.bias + j), BF16);
+        if (p.Z) p.Z[token * p.ld_z + j] = static_cast<uint16_t>(half_bits(z, BF16));
+        float y = activate(z, p.act);
+        if (p.residual) y += half_value(ld_u16(p.residual + token * p.ld_r + j), BF16);
+        p.out[token * p.ld_out + j] = static_cast<uint16_t>(half_bits(y, BF16));
+    }
+    if (ranks > 1) cluster_sync_all();                            // nobody leaves while its shared memory is read
+}
+
+// ------------------------------------------------------------------------------------------------ tensor cores
+constexpr int LP_STAGES = 6;
+constexpr int LP_SLOT_BYTES = (CTA_ROWS / BOX_FEATURES) * BOX_BYTES;      // one operand block: 16 KB
+constexpr int LP_STAGE_BYTES = 2 * LP_SLOT_BYTES;                         // [weights | tokens]
+constexpr int LP_LOOK_WARPS = 8;                                          // two groups of four, every other k-step each
+constexpr int LP_EPI_WARPS = 8;
+constexpr int LP_THREADS = 32 * (4 + LP_LOOK_WARPS + LP_EPI_WARPS);
+constexpr int LP_SMEM_BYTES = LP_STAGES * LP_STAGE_BYTES + 1024;
+constexpr int LG_STAGES = 6;                                              // gradient of the levels: [dZ | tokens]
+constexpr int LG_SMEM_BYTES = LG_STAGES * LP_STAGE_BYTES + LP_EPI_WARPS * LIN_LEVELS * 32 * 4 + 1024;
+constexpr int LG_THREADS = 32 * (4 + LP_EPI_WARPS);
+constexpr int LG_CHUNK_KSTEPS = 16;                                       // 1024 tokens
+constexpr int LP_ROW_BLOCK = 16;                                          // row tiles that are worked on beside each other
+
+// K-major operand with the 128-byte swizzle: rows of 128 bytes (64 contraction indices), groups of 8 rows 1024 bytes apart; the next 16
+// contraction indices are 32 bytes further.
+__device__ __forceinline__ uint64_t umma_smem_desc_k_sw128(uint32_t smem_addr)
+{
+    uint64_t d = 0;
+    d |= static_cast<uint64_t>((smem_addr & 0x3FFFFu) >> 4);
+    d |= static_cast<uint64_t>(1) << 16;
+    d |= static_cast<uint64_t>(1024 >> 4) << 32;
+    d |= static_cast<uint64_t>(1) << 46;
+    d |= static_cast<uint64_t>(2) << 61;
+    return d;
+}
+// kind::f16 with fp32 accumulation, A and B both bf16 or both fp16.
+__host__ __device__ constexpr uint32_t umma_idesc_16(uint32_t m, uint32_t n, bool bf16, bool a_mn, bool b_mn)
+{
+    return (1u << 4) | ((bf16 ? 1u : 0u) << 7) | ((bf16 ? 1u : 0u) << 10) | ((a_mn ? 1u : 0u) << 15) | ((b_mn ? 1u : 0u) << 16) |
+           ((n >> 3) << 17) | ((m >> 4) << 24);
+}
+
+struct LinearUnit {
+    int row0, tok0;
+};
+// The it-th tile of a pair.  Row tiles in blocks of LP_ROW_BLOCK, inside a block token tiles outermost: tiles worked on at the same time
+// share few token tiles (2 bytes an element) and more row tiles (half a byte).
+__device__ __forceinline__ bool linear_unit(const LinearParams &p, int pair, int it, LinearUnit &u)
+{
+    const int unit = it * p.pairs + pair;
+    if (unit >= p.units) return false;
+    const int per = LP_ROW_BLOCK * p.tok_tiles, block = unit / per, rest = unit - block * per;
+    const int left = p.row_tiles - block * LP_ROW_BLOCK, width = left < LP_ROW_BLOCK ? left : LP_ROW_BLOCK;
+    const int tok = rest / width;
+    u.row0 = (block * LP_ROW_BLOCK + rest - tok * width) * TILE_M;
+    u.tok0 = tok * TILE_N;
+    return true;
+}
+
+// Forward (BACK false): D[channel][token] = sum_c W[channel][c] X[token][c], both operands with the contraction contiguous; a lookup thread
+// owns a channel for the whole tile, its levels stay in registers.  Backward: D[c][token] = sum_j W[j][c] dZ[token][j]; the rows of
+// the weight operand are contraction indices, a lookup thread owns 64 columns of one channel a k-step and fetches that
+// channel's levels with the codes.  The codes of a thread's next k-step are read while it looks the present ones up.
+// Rows of D are the lanes of tensor memory, so tokens (columns) come in any number without work for the weights' side.
+template <bool BACK, bool WIDE>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LP_THREADS, 1)
+linear_pair_kernel(const __grid_constant__ CUtensorMap mapX, const LinearParams p)
+{
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ __align__(8) uint64_t bar_full[LP_STAGES];     // first CTA: bytes of both CTAs + four lookup warps of both
+    __shared__ __align__(8) uint64_t bar_empty[LP_STAGES];    // both CTAs: signalled by the MMA commits
+    __shared__ __align__(8) uint64_t bar_acc_full[2];         // both CTAs, one per accumulator
+    __shared__ __align__(8) uint64_t bar_acc_empty[2];        // first CTA, one per accumulator: 16 epilogue warps arrive
+    __shared__ __align__(8) uint64_t bar_drain;
+    __shared__ uint32_t tmem_base_smem;
+    __shared__ volatile uint32_t abort_flag;
+
+    const int warp = threadIdx.x >> 5;
+    const int lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_ctarank();
+    const int pair = static_cast<int>(blockIdx.x >> 1);
+    const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    const int kdim = BACK ? p.d_out : p.d_in, rows = BACK ? p.d_in : p.d_out;
+    const int kblocks = (kdim + TILE_K - 1) / TILE_K;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < LP_STAGES; ++s) {
+            mbar_init(smem_u32(&bar_full[s]), 1 + LP_LOOK_WARPS);
+            mbar_init(smem_u32(&bar_empty[s]), 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(smem_u32(&bar_acc_full[b]), 1);
+            mbar_init(smem_u32(&bar_acc_empty[b]), 2 * LP_EPI_WARPS);
+        }
+        mbar_init(smem_u32(&bar_drain), 1);
+        abort_flag = 0u;
+        fence_mbar_init();
+        prefetch_tensormap(&mapX);
+    }
+    griddep_launch();
+    if (warp == 2) {
+        tmem_alloc(smem_u32(&tmem_base_smem), TMEM_COLS);
+        tmem_relinquish();
+    }
+    tc_fence_before_sync();
+    cluster_sync_all();
+    tc_fence_after_sync();
+    const uint32_t tmem_base = tmem_base_smem;
+    const WaitCtx wc{&abort_flag, p.status, p.wait_budget_ns};
+    griddep_wait();
+
+    if (warp == 0 && lane == 0) {
+        // ------------------------------------------------------------------ TMA producer (both CTAs): tokens
+        int s = 0;
+        uint32_t ph = 0;
+        uint32_t issued = 0;
+        bool ok = true;
+        LinearUnit u;
+        for (int it = 0; ok && linear_unit(p, pair, it, u); ++it) {
+            const int b0 = u.tok0 + static_cast<int>(rank) * CTA_ROWS;
+            for (int kb = 0; kb < kblocks; ++kb) {
+                if (!bounded_wait(smem_u32(&bar_empty[s]), ph ^ 1u, wc, 1u, it)) { ok = false; break; }
+                const uint32_t full_local = smem_u32(&bar_full[s]);
+                if (rank == 0) mbar_arrive_expect_tx(full_local, 2 * LP_SLOT_BYTES);      // both CTAs' bytes
+                const uint32_t full = map_to_cta(full_local, 0);
+                const uint32_t stage = ring + s * LP_STAGE_BYTES;
+#pragma unroll
+                for (int q = 0; q < CTA_ROWS / TILE_K; ++q)
+                    tma_load_3d_pair(stage + LP_SLOT_BYTES + q * BOX_BYTES, &mapX, full, kb * TILE_K, b0 + q * TILE_K, 0);
+                ++issued;
+                if (++s == LP_STAGES) { s = 0; ph ^= 1u; }
+            }
+        }
+        // Stay until every stage has been released again: the release is an arrival on this CTA's barriers,
+        // which must not come after the CTA has gone.
+        for (int q = 0; ok && issued != 0u && q < LP_STAGES; ++q) {
+            if (!bounded_wait(smem_u32(&bar_empty[s]), ph ^ 1u, wc, 5u, 0u)) ok = false;
+            if (++s == LP_STAGES) { s = 0; ph ^= 1u; }
+        }
+        if (!ok) spin_ns(1000000ull);
+    } else if (warp == 3 && lane == 0 && rank == 0) {
+        // ------------------------------------------------------------------ MMA issuer (first CTA)
+        const uint32_t idesc = umma_idesc_16(TILE_M, TILE_N, p.bf16 != 0, BACK, false);
+        int s = 0;
+        uint32_t ph = 0;
+        uint32_t acc_ph = 0u;                           // bit b: phase of accumulator b
+        int buf = 0;
+        bool ok = true;
+        LinearUnit u;
+        for (int it = 0; ok && linear_unit(p, pair, it, u); ++it) {
+            if (!bounded_wait_hot(smem_u32(&bar_acc_empty[buf]), ((acc_ph >> buf) & 1u) ^ 1u, wc, 2u, it)) { ok = false; break; }
+            tc_fence_after_sync();
+            const uint32_t d_tmem = tmem_base + static_cast<uint32_t>(buf * TILE_N);
+            for (int kb = 0; kb < kblocks; ++kb) {
+                if (!bounded_wait_hot(smem_u32(&bar_full[s]), ph, wc, 3u, it)) { ok = false; break; }
+                tc_fence_after_sync();
+                const uint32_t sa = ring + s * LP_STAGE_BYTES;
+                const uint32_t sb = sa + LP_SLOT_BYTES;
+#pragma unroll
+                for (int k16 = 0; k16 < TILE_K / 16; ++k16) {
+                    const uint64_t adesc = BACK ? umma_smem_desc_mn_sw128(sa + k16 * 16 * 128, BOX_BYTES, 1024) : umma_smem_desc_k_sw128(sa + k16 * 32);
+                    const uint64_t bdesc = umma_smem_desc_k_sw128(sb + k16 * 32);
+                    umma_bf16(d_tmem, adesc, bdesc, idesc, (kb != 0 || k16 != 0) ? 1u : 0u);
+                }
+                umma_commit_pair(smem_u32(&bar_empty[s]));
+                if (++s == LP_STAGES) { s = 0; ph ^= 1u; }
+            }
+            if (!ok) break;
+            umma_commit_pair(smem_u32(&bar_acc_full[buf]));
+            acc_ph ^= 1u << buf;
+            buf ^= 1;
+        }
+        if (!ok) {
+            // Make sure no MMA is still writing TMEM when it is released.
+            umma_commit_local(smem_u32(&bar_drain));
+            const uint64_t t0 = global_timer_ns();
+            while (!mbar_try_wait(smem_u32(&bar_drain), 0u) && global_timer_ns() - t0 < 5000000ull) {}
+        }
+    } else if (warp >= 4 && warp < 4 + LP_LOOK_WARPS) {
+        // ------------------------------------------------------------------ weight operand
+        const int grp = (warp - 4) >> 2;                            // takes k-steps grp, grp + 2, ... of the launch
+        const int r = ((warp - 4) & 3) * 32 + lane;                 // forward: channel; backward: channel r % 64, columns 64 (r / 64) ..
+        const uint32_t slot = BACK ? static_cast<uint32_t>((r >> 6) * BOX_BYTES + (r & 63) * 128) : static_cast<uint32_t>(r * 128);
+        const uint32_t xor7 = static_cast<uint32_t>(r & 7);
+        struct Fetch {
+            uint4 c[2], t[2];
+        };
+        auto fetch = [&](const LinearUnit &u, int kb, Fetch &f) {
+            const int row = u.row0 + static_cast<int>(rank) * CTA_ROWS + (BACK ? (r >> 6) * 64 : r);
+            const int j = BACK ? kb * TILE_K + (r & 63) : row;
+            const int byte = (BACK ? row : kb * TILE_K) >> 1;
+            const bool in = j < p.d_out;
+            const uint8_t *at = p.codes + static_cast<size_t>(in ? j : 0) * p.ld_codes + byte;
+#pragma unroll
+            for (int q = 0; q < 2; ++q)
+                f.c[q] = (in && byte + 16 * q < p.ld_codes) ? ld_u32x4(at + 16 * q) : make_uint4(0u, 0u, 0u, 0u);
+            if (BACK) {
+                const uint4 *tb = reinterpret_cast<const uint4 *>(p.table + static_cast<size_t>(in ? j : 0) * LIN_LEVELS);
+#pragma unroll
+                for (int q = 0; q < 2; ++q) f.t[q] = in ? ld_u32x4(tb + q) : make_uint4(0u, 0u, 0u, 0u);
+            }
+        };
+        LevelPlanes lv;
+        int s = grp;
+        uint32_t ph = 0;
+        int kb = grp;                                               // next k-step of this group
+        bool ok = true;
+        LinearUnit u, un;
+        int it = 0;
+        bool valid = linear_unit(p, pair, 0, u);
+        while (valid && kb >= kblocks) {                            // kblocks may be 1
+            kb -= kblocks;
+            valid = linear_unit(p, pair, ++it, u);
+        }
+        Fetch cur, next;
+        if (valid) fetch(u, kb, cur);
+        bool fresh = true;                                          // a new tile: the channel's levels
+        while (valid) {
+            if (!BACK && fresh) {
+                const int j = u.row0 + static_cast<int>(rank) * CTA_ROWS + r;
+                const uint4 *tb = reinterpret_cast<const uint4 *>(p.table + static_cast<size_t>(j < p.d_out ? j : 0) * LIN_LEVELS);
+                const uint4 t0 = ld_u32x4(tb), t1 = ld_u32x4(tb + 1);
+                lv.set(t0, t1);
+            }
+            // the k-step after this one
+            int kn = kb + 2, itn = it;
+            bool vn = true;
+            un = u;
+            while (vn && kn >= kblocks) {
+                kn -= kblocks;
+                vn = linear_unit(p, pair, ++itn, un);
+            }
+            if (vn) fetch(un, kn, next);
+            if (BACK) lv.set(cur.t[0], cur.t[1]);
+            bool got = true;
+            if (lane == 0) got = bounded_wait(smem_u32(&bar_empty[s]), ph ^ 1u, wc, 6u, it);
+            got = __any_sync(0xffffffffu, got && lane == 0);
+            if (!got) { ok = false; break; }
+            (void)mbar_try_wait(smem_u32(&bar_empty[s]), ph ^ 1u);           // every lane observes the completed phase
+            const uint32_t base = ring + s * LP_STAGE_BYTES + slot;
+            const bool ragged = !BACK && (kb + 1) * TILE_K > kdim;
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                const uint32_t w[4] = {cur.c[q].x, cur.c[q].y, cur.c[q].z, cur.c[q].w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    uint4 v = lv.look<WIDE>(w[e]);
+                    if (ragged && kb * TILE_K + 32 * q + 8 * e >= kdim) v = make_uint4(0u, 0u, 0u, 0u);      // no level meets padding
+                    st_shared_16(base + ((static_cast<uint32_t>(4 * q + e) ^ xor7) << 4), v);
+                }
+            }
+            fence_proxy_async_smem();                // make the stores visible to the tensor core's reads
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(map_to_cta(smem_u32(&bar_full[s]), 0));
+            s += 2;
+            if (s >= LP_STAGES) { s -= LP_STAGES; ph ^= 1u; }
+            fresh = itn != it;
+            kb = kn;
+            it = itn;
+            u = un;
+            valid = vn;
+            cur = next;
+        }
+        (void)ok;
+    } else if (warp >= 4 + LP_LOOK_WARPS) {
+        // ------------------------------------------------------------------ epilogue: bias, activation, residual, rounding
+        const int ew = warp - (4 + LP_LOOK_WARPS);      // 0..7; four consecutive warps cover the four lane quarters
+        const int q = warp & 3;                         // TMEM lane quarter this warp may access
+        const int half = ew >> 2;                       // which 128 of the 256 tokens
+        const bool bf16 = p.bf16 != 0;
+        uint32_t full_ph = 0u;                          // bit b: phase of accumulator b
+        int buf = 0;
+        bool ok = true;
+        LinearUnit u;
+        for (int it = 0; ok && linear_unit(p, pair, it, u); ++it) {
+            if (lane == 0) ok = bounded_wait(smem_u32(&bar_acc_full[buf]), (full_ph >> buf) & 1u, wc, 4u, it);
+            ok = __shfl_sync(0xffffffffu, ok, 0);
+            if (!ok) break;
+            (void)mbar_try_wait(smem_u32(&bar_acc_full[buf]), (full_ph >> buf) & 1u);     // every lane observes the completed phase
+            full_ph ^= 1u << buf;
+            tc_fence_after_sync();
+            const uint32_t tmem_tile = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + static_cast<uint32_t>(buf * TILE_N + half * 128);
+            const int row = u.row0 + static_cast<int>(rank) * CTA_ROWS + q * 32 + lane;
+            const bool in = row < rows;
+            float bias = 0.0f;
+            if (!BACK && p.bias && in) bias = half_value(ld_u16(p.bias + row), bf16);
+            // Lanes 2 i and 2 i + 1 exchange every other token, so that each holds two neighbouring rows of a token: 4-byte accesses.
+            const int odd = lane & 1, pair_row = row - odd;
+#pragma unroll 1
+            for (int n0 = 0; n0 < 128; n0 += 32) {
+                uint32_t acc[32];
+                tmem_ld_32x32(tmem_tile + static_cast<uint32_t>(n0), acc);
+                tmem_ld_wait();
+                if (n0 == 96) {
+                    tc_fence_before_sync();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_cluster(map_to_cta(smem_u32(&bar_acc_empty[buf]), 0));
+                }
+                const int tok0 = u.tok0 + half * 128 + n0;
+                if (tok0 >= p.n) continue;
+#pragma unroll
+                for (int e = 0; e < 32; e += 2) {
+                    float v0 = __uint_as_float(acc[e]) + bias, v1 = __uint_as_float(acc[e + 1]) + bias;
+                    const float other = __shfl_xor_sync(0xffffffffu, odd ? v0 : v1, 1);
+                    if (odd) v0 = other;
+                    else v1 = other;
+                    // even lane: token e of rows (row, row + 1); odd lane: token e + 1 of rows (row - 1, row)
+                    const int token = tok0 + e + odd;
+                    if (in && token < p.n) {
+                        if (!BACK) {
+                            if (p.Z) *reinterpret_cast<uint32_t *>(p.Z + token * p.ld_z + pair_row) = half2_bits(v0, v1, bf16);
+                            v0 = activate(v0, p.act);
+                            v1 = activate(v1, p.act);
+                            if (p.residual) {
+                                const float2 res = half2_value(*reinterpret_cast<const uint32_t *>(p.residual + token * p.ld_r + pair_row), bf16);
+                                v0 += res.x;
+                                v1 += res.y;
+                            }
+                        }
+                        *reinterpret_cast<uint32_t *>(p.out + token * p.ld_out + pair_row) = half2_bits(v0, v1, bf16);
+                    }
+                }
+            }
+            buf ^= 1;
+        }
+    }
+
+    __syncwarp();
+    tc_fence_before_sync();
+    cluster_sync_all();
+    if (warp == 2) {
+        tc_fence_after_sync();
+        tmem_dealloc(tmem_base, TMEM_COLS);
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ backward pass
+constexpr int LZ_COLUMNS = 256;           // columns of a block: 32 lanes x 8
+constexpr int LZ_WARPS = 8;
+constexpr int LZ_MIN_ROWS = 64;           // rows of a block, more where there would be too many blocks
+constexpr int LZ_MAX_BLOCKS = 256;
+
+// dz = dy act'(z), rounded to the activations' type, and per block of rows the column sums of the rounded values (db is their sum over
+// the blocks, in the blocks' order).  Without an activation dZ is null: dy is dz, only the sums are formed.
+__global__ void __launch_bounds__(32 * LZ_WARPS) linear_dz_kernel(const uint16_t *dY, long long ld_dy, const uint16_t *Z, long long ld_z, int act, int bf16,
+                                                                  int n, int d_out, int rows_per_block, uint16_t *dZ, long long ld_dz, float *col_sums)
+{
+    __shared__ float part[LZ_WARPS][LZ_COLUMNS];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int col = static_cast<int>(blockIdx.x) * LZ_COLUMNS + lane * 8;
+    const int r0 = static_cast<int>(blockIdx.y) * rows_per_block, r1 = min(r0 + rows_per_block, n);
+    griddep_launch();
+    griddep_wait();
+    float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (col < d_out) {
+        for (int i = r0 + warp; i < r1; i += LZ_WARPS) {
+            const uint4 y = ld_u32x4(dY + i * ld_dy + col);
+            const uint32_t *yw = reinterpret_cast<const uint32_t *>(&y);
+            if (dZ) {
+                const uint4 z = ld_u32x4(Z + i * ld_z + col);
+                const uint32_t *zw = reinterpret_cast<const uint32_t *>(&z);
+                uint4 out;
+                uint32_t *ow = reinterpret_cast<uint32_t *>(&out);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float2 a = half2_value(yw[e], bf16 != 0), b = half2_value(zw[e], bf16 != 0);
+                    ow[e] = half2_bits(a.x * activation_slope(b.x, act), a.y * activation_slope(b.y, act), bf16 != 0);
+                    const float2 kept = half2_value(ow[e], bf16 != 0);
+                    sum[2 * e] += kept.x;
+                    sum[2 * e + 1] += kept.y;
+                }
+                *reinterpret_cast<uint4 *>(dZ + i * ld_dz + col) = out;
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float2 a = half2_value(yw[e], bf16 != 0);
+                    sum[2 * e] += a.x;
+                    sum[2 * e + 1] += a.y;
+                }
+            }
+        }
+    }
+    if (!col_sums) return;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) part[warp][lane * 8 + e] = sum[e];
+    __syncthreads();
+    const int c = static_cast<int>(blockIdx.x) * LZ_COLUMNS + static_cast<int>(threadIdx.x);
+    if (c < d_out) {
+        float total = 0.0f;
+#pragma unroll
+        for (int w = 0; w < LZ_WARPS; ++w) total += part[w][threadIdx.x];
+        col_sums[static_cast<size_t>(blockIdx.y) * d_out + c] = total;
+    }
+}
+
+struct LevelGradParams {
+    const uint8_t *codes;
+    int ld_codes;
+    int n, d_in, d_out;
+    int bf16;
+    int ch_tiles, f_tiles, chunks;       // tiles of 256 channels and 256 features, pieces of the tokens
+    int chunk_ksteps;                    // k-steps (of 64 tokens) of a piece
+    int runs;                            // pieces of a channel tile's f_tiles * chunks units, a partial sum each
+    int pairs;
+    float *partial;                      // [runs][2][d_out][16]
+    uint32_t *status;
+    unsigned long long wait_budget_ns;
+};
+
+struct LevelGradUnit {
+    int tile, run, f0, t0, t1;           // channel tile, run, first feature, k-steps [t0, t1)
+    bool last;                           // of its run
+};
+// The units of a pair: runs pair, pair + pairs, ... of ch_tiles * runs, and within a run its share of (feature tile, token piece).
+struct LevelGradCursor {
+    const LevelGradParams &p;
+    int item, unit, end;
+    __device__ LevelGradCursor(const LevelGradParams &pp, int pair) : p(pp), item(pair), unit(0), end(0) { open(); }
+    __device__ void open()
+    {
+        const int total = p.f_tiles * p.chunks, run = item % p.runs;
+        unit = static_cast<int>(static_cast<long long>(total) * run / p.runs);
+        end = static_cast<int>(static_cast<long long>(total) * (run + 1) / p.runs);
+    }
+    __device__ bool next(LevelGradUnit &u)
+    {
+        if (unit == end) {
+            item += p.pairs;
+            open();
+        }
+        if (item >= p.ch_tiles * p.runs) return false;
+        u.tile = item / p.runs;
+        u.run = item % p.runs;
+        const int f = unit / p.chunks, c = unit - f * p.chunks;
+        const int ksteps = (p.n + TILE_K - 1) / TILE_K;
+        u.f0 = f * TILE_N;
+        u.t0 = c * p.chunk_ksteps;
+        u.t1 = min(u.t0 + p.chunk_ksteps, ksteps);
+        u.last = ++unit == end;
+        return true;
+    }
+};
+
+// Gradient of the levels: G[j][c] = sum_i dz_ij x_ic on the tensor cores (both operands by TMA, tokens as rows), never in memory: a lane
+// of the epilogue is a channel and adds its entries to the sum of the level their code names, in shared memory.  A pair keeps these
+// sums over a run of tiles and writes 16 numbers a channel at its end; the runs are added up in their order by linear_sum_kernel.
+// The tokens are taken in pieces of at most 1024: the tensor cores' accumulation truncates, so that long runs drift.
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LG_THREADS, 1)
+linear_level_grad_kernel(const __grid_constant__ CUtensorMap mapG, const __grid_constant__ CUtensorMap mapX, const LevelGradParams p)
+{
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ __align__(8) uint64_t bar_full[LG_STAGES];     // first CTA: bytes of both CTAs
+    __shared__ __align__(8) uint64_t bar_empty[LG_STAGES];    // both CTAs: signalled by the MMA commits
+    __shared__ __align__(8) uint64_t bar_acc_full[2];         // both CTAs, one per accumulator
+    __shared__ __align__(8) uint64_t bar_acc_empty[2];        // first CTA, one per accumulator: 16 epilogue warps arrive
+    __shared__ __align__(8) uint64_t bar_drain;
+    __shared__ uint32_t tmem_base_smem;
+    __shared__ volatile uint32_t abort_flag;
+
+    const int warp = threadIdx.x >> 5;
+    const int lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_ctarank();
+    const int pair = static_cast<int>(blockIdx.x >> 1);
+    const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < LG_STAGES; ++s) {
+            mbar_init(smem_u32(&bar_full[s]), 1);
+            mbar_init(smem_u32(&bar_empty[s]), 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(smem_u32(&bar_acc_full[b]), 1);
+            mbar_init(smem_u32(&bar_acc_empty[b]), 2 * LP_EPI_WARPS);
+        }
+        mbar_init(smem_u32(&bar_drain), 1);
+        abort_flag = 0u;
+        fence_mbar_init();
+        prefetch_tensormap(&mapG);
+        prefetch_tensormap(&mapX);
+    }
+    griddep_launch();
+    if (warp == 2) {
+        tmem_alloc(smem_u32(&tmem_base_smem), TMEM_COLS);
+        tmem_relinquish();
+    }
+    tc_fence_before_sync();
+    cluster_sync_all();
+    tc_fence_after_sync();
+    const uint32_t tmem_base = tmem_base_smem;
+    const WaitCtx wc{&abort_flag, p.status, p.wait_budget_ns};
+    griddep_wait();
+
+    if (warp == 0 && lane == 0) {
+        // ------------------------------------------------------------------ TMA producer (both CTAs)
+        int s = 0;
+        uint32_t ph = 0;
+        uint32_t issued = 0;
+        bool ok = true;
+        LevelGradCursor cur(p, pair);
+        LevelGradUnit u;
+        while (ok && cur.next(u)) {
+            const int a0 = u.tile * TILE_M + static_cast<int>(rank) * CTA_ROWS, b0 = u.f0 + static_cast<int>(rank) * CTA_ROWS;
+            for (int kb = u.t0; kb < u.t1; ++kb) {
+                if (!bounded_wait(smem_u32(&bar_empty[s]), ph ^ 1u, wc, 1u, u.tile)) { ok = false; break; }
+                const uint32_t full_local = smem_u32(&bar_full[s]);
+                if (rank == 0) mbar_arrive_expect_tx(full_local, 4 * LP_SLOT_BYTES);      // both CTAs' bytes
+                const uint32_t full = map_to_cta(full_local, 0);
+                const uint32_t stage = ring + s * LP_STAGE_BYTES;
+#pragma unroll
+                for (int q = 0; q < CTA_ROWS / BOX_FEATURES; ++q) {
+                    tma_load_3d_pair(stage + q * BOX_BYTES, &mapG, full, a0 + q * BOX_FEATURES, kb * TILE_K, 0);
+                    tma_load_3d_pair(stage + LP_SLOT_BYTES + q * BOX_BYTES, &mapX, full, b0 + q * BOX_FEATURES, kb * TILE_K, 0);
+                }
+                ++issued;
+                if (++s == LG_STAGES) { s = 0; ph ^= 1u; }
+            }
+        }
+        // Stay until every stage has been released again (see linear_pair_kernel).
+        for (int q = 0; ok && issued != 0u && q < LG_STAGES; ++q) {
+            if (!bounded_wait(smem_u32(&bar_empty[s]), ph ^ 1u, wc, 5u, 0u)) ok = false;
+            if (++s == LG_STAGES) { s = 0; ph ^= 1u; }
+        }
+        if (!ok) spin_ns(1000000ull);
+    } else if (warp == 3 && lane == 0 && rank == 0) {
+        // ------------------------------------------------------------------ MMA issuer (first CTA)
+        const uint32_t idesc = umma_idesc_16(TILE_M, TILE_N, p.bf16 != 0, true, true);
+        int s = 0;
+        uint32_t ph = 0;
+        uint32_t acc_ph = 0u;                           // bit b: phase of accumulator b
+        int buf = 0;
+        bool ok = true;
+        LevelGradCursor cur(p, pair);
+        LevelGradUnit u;
+        while (ok && cur.next(u)) {
+            if (!bounded_wait_hot(smem_u32(&bar_acc_empty[buf]), ((acc_ph >> buf) & 1u) ^ 1u, wc, 2u, u.tile)) { ok = false; break; }
+            tc_fence_after_sync();
+            const uint32_t d_tmem = tmem_base + static_cast<uint32_t>(buf * TILE_N);
+            for (int kb = u.t0; kb < u.t1; ++kb) {
+                if (!bounded_wait_hot(smem_u32(&bar_full[s]), ph, wc, 3u, u.tile)) { ok = false; break; }
+                tc_fence_after_sync();
+                const uint32_t sa = ring + s * LP_STAGE_BYTES;
+                const uint32_t sb = sa + LP_SLOT_BYTES;
+#pragma unroll
+                for (int k16 = 0; k16 < TILE_K / 16; ++k16) {
+                    const uint64_t adesc = umma_smem_desc_mn_sw128(sa + k16 * 16 * 128, BOX_BYTES, 1024);
+                    const uint64_t bdesc = umma_smem_desc_mn_sw128(sb + k16 * 16 * 128, BOX_BYTES, 1024);
+                    umma_bf16(d_tmem, adesc, bdesc, idesc, (kb != u.t0 || k16 != 0) ? 1u : 0u);
+                }
+                umma_commit_pair(smem_u32(&bar_empty[s]));
+                if (++s == LG_STAGES) { s = 0; ph ^= 1u; }
+            }
+            if (!ok) break;
+            umma_commit_pair(smem_u32(&bar_acc_full[buf]));
+            acc_ph ^= 1u << buf;
+            buf ^= 1;
+        }
+        if (!ok) {
+            // Make sure no MMA is still writing TMEM when it is released.
+            umma_commit_local(smem_u32(&bar_drain));
+            const uint64_t t0 = global_timer_ns();
+            while (!mbar_try_wait(smem_u32(&bar_drain), 0u) && global_timer_ns() - t0 < 5000000ull) {}
+        }
+    } else if (warp >= 4 && warp < 4 + LP_EPI_WARPS) {
+        // ------------------------------------------------------------------ epilogue: sums by level
+        const int ew = warp - 4;                        // 0..7; four consecutive warps cover the four lane quarters
+        const int q = warp & 3;                         // TMEM lane quarter this warp may access
+        const int half = ew >> 2;                       // which 128 of the 256 features
+        float *sums = reinterpret_cast<float *>(smem_raw + (ring - smem_u32(smem_raw)) + LG_STAGES * LP_STAGE_BYTES) + ew * LIN_LEVELS * 32 + lane;
+#pragma unroll
+        for (int l = 0; l < LIN_LEVELS; ++l) sums[l * 32] = 0.0f;
+        uint32_t full_ph = 0u;                          // bit b: phase of accumulator b
+        int buf = 0;
+        bool ok = true;
+        LevelGradCursor cur(p, pair);
+        LevelGradUnit u;
+        while (ok && cur.next(u)) {
+            const int j = u.tile * TILE_M + static_cast<int>(rank) * CTA_ROWS + q * 32 + lane;
+            const bool have = j < p.d_out;
+            const int byte0 = (u.f0 + half * 128) >> 1;
+            const uint8_t *row = p.codes + static_cast<size_t>(have ? j : 0) * p.ld_codes;
+            uint4 codes[4];                             // 128 features
+#pragma unroll
+            for (int x = 0; x < 4; ++x) codes[x] = byte0 + 16 * x < p.ld_codes ? ld_u32x4(row + byte0 + 16 * x) : make_uint4(0u, 0u, 0u, 0u);
+            if (lane == 0) ok = bounded_wait(smem_u32(&bar_acc_full[buf]), (full_ph >> buf) & 1u, wc, 4u, u.tile);
+            ok = __shfl_sync(0xffffffffu, ok, 0);
+            if (!ok) break;
+            (void)mbar_try_wait(smem_u32(&bar_acc_full[buf]), (full_ph >> buf) & 1u);     // every lane observes the completed phase
+            full_ph ^= 1u << buf;
+            tc_fence_after_sync();
+            const uint32_t tmem_tile = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + static_cast<uint32_t>(buf * TILE_N + half * 128);
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                uint32_t acc[32];
+                tmem_ld_32x32(tmem_tile + static_cast<uint32_t>(32 * x), acc);
+                tmem_ld_wait();
+                if (x == 3) {
+                    tc_fence_before_sync();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_cluster(map_to_cta(smem_u32(&bar_acc_empty[buf]), 0));
+                }
+                const uint32_t w[4] = {codes[x].x, codes[x].y, codes[x].z, codes[x].w};
+                // features behind d_in: their column of G is zero and so is their code
+#pragma unroll
+                for (int e = 0; e < 32; ++e) sums[((w[e >> 3] >> (4 * (e & 7))) & 15u) * 32] += __uint_as_float(acc[e]);
+            }
+            if (u.last) {
+                float v[LIN_LEVELS];
+#pragma unroll
+                for (int l = 0; l < LIN_LEVELS; ++l) {
+                    v[l] = sums[l * 32];
+                    sums[l * 32] = 0.0f;
+                }
+                if (have) {
+                    float4 *out = reinterpret_cast<float4 *>(p.partial + ((static_cast<size_t>(u.run) * 2 + half) * p.d_out + j) * LIN_LEVELS);
+#pragma unroll
+                    for (int l = 0; l < LIN_LEVELS / 4; ++l) out[l] = make_float4(v[4 * l], v[4 * l + 1], v[4 * l + 2], v[4 * l + 3]);
+                }
+            }
+            buf ^= 1;
+        }
+    }
+
+    __syncwarp();
+    tc_fence_before_sync();
+    cluster_sync_all();
+    if (warp == 2) {
+        tc_fence_after_sync();
+        tmem_dealloc(tmem_base, TMEM_COLS);
+    }
+}
+
+// Sums of the partial results in their order, in 64 bits: d_table [d_out][m] from `parts` parts, d_bias [d_out] from `blocks` rows.
+__global__ void __launch_bounds__(256) linear_sum_kernel(const float *partial, int parts, int d_out, int m, float *d_table, const float *col_sums,
+                                                         int blocks, float *d_bias)
+{
+    griddep_launch();
+    griddep_wait();
+    const long long i = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x, cells = static_cast<long long>(d_out) * LIN_LEVELS;
+    if (i < cells) {
+        if (!d_table) return;
+        const int j = static_cast<int>(i / LIN_LEVELS), l = static_cast<int>(i % LIN_LEVELS);
+        if (l >= m) return;
+        double total = 0.0;
+        for (int r = 0; r < parts; ++r) total += static_cast<double>(partial[static_cast<size_t>(r) * cells + i]);
+        d_table[static_cast<size_t>(j) * m + l] = static_cast<float>(total);
+    } else if (i - cells < d_out && d_bias) {
+        double total = 0.0;
+        for (int b = 0; b < blocks; ++b) total += static_cast<double>(col_sums[static_cast<size_t>(b) * d_out + (i - cells)]);
+        d_bias[i - cells] = static_cast<float>(total);
+    }
+}
+
+}  // namespace gq
