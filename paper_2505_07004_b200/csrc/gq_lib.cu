@@ -287,6 +287,23 @@ int32_t make_map_f32(CUtensorMap *map, const float *base, int64_t cols, int64_t 
     return GQ_OK;
 }
 
+// Bytes [rows][width] (width a multiple of 16) as a TMA map with boxes of `box_width` bytes x `box_rows` rows.
+int32_t make_map_bytes(CUtensorMap *map, const void *base, int64_t width, int64_t rows, int box_width, int box_rows)
+{
+    cuuint64_t dims[3] = {static_cast<cuuint64_t>(width), static_cast<cuuint64_t>(rows), 1};
+    cuuint64_t strides[2] = {static_cast<cuuint64_t>(width), static_cast<cuuint64_t>(width) * static_cast<cuuint64_t>(rows)};
+    cuuint32_t box[3] = {static_cast<cuuint32_t>(box_width), static_cast<cuuint32_t>(box_rows), 1};
+    cuuint32_t estr[3] = {1, 1, 1};
+    CUresult r = g_encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void *>(base), dims, strides, box, estr,
+                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) {
+        tl_last_cuda_error = static_cast<int32_t>(cudaErrorInvalidValue);
+        return GQ_ERR_CUDA;
+    }
+    return GQ_OK;
+}
+
 // H [groups][d][d] with 32 x 32 boxes and the 128-byte swizzle (reduce-add target).
 int32_t make_map_h(CUtensorMap *map, float *H, int64_t d, int64_t groups)
 {
@@ -1475,13 +1492,15 @@ static int32_t linear_pair(bool back, gq::LinearParams p, int32_t dtype, const v
     p.pairs = p.units < di->max_pairs ? p.units : di->max_pairs;
     p.status = di->status_ptr;
     p.wait_budget_ns = wait_budget_ns();
-    CUtensorMap map;
+    CUtensorMap map, map_codes;
     if (int32_t rc = make_map(&map, in, kdim, p.n, 1, ld_in, static_cast<int64_t>(p.n) * ld_in, map_type(dtype))) return rc;
+    // a k-step's codes: 128 channels x 32 bytes forward, 64 channels x 64 bytes backward
+    if (int32_t rc = make_map_bytes(&map_codes, p.codes, p.ld_codes, p.d_out, back ? 64 : 32, back ? gq::TILE_K : gq::CTA_ROWS)) return rc;
     {
         LaunchScope scope(GQ_KERNEL_LINEAR, st);
         const auto kernel = back ? (m > 8 ? gq::linear_pair_kernel<true, true> : gq::linear_pair_kernel<true, false>)
                                  : (m > 8 ? gq::linear_pair_kernel<false, true> : gq::linear_pair_kernel<false, false>);
-        launch(kernel, dim3(static_cast<unsigned>(2 * p.pairs)), gq::LP_THREADS, gq::LP_SMEM_BYTES, st, map, p);
+        launch(kernel, dim3(static_cast<unsigned>(2 * p.pairs)), gq::LP_THREADS, gq::LP_SMEM_BYTES, st, map, map_codes, p);
     }
     GQ_CUDA(cudaGetLastError());
     return GQ_OK;

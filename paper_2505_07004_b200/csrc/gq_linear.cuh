@@ -36,6 +36,22 @@ __device__ __forceinline__ uint4 ld_u32x4(const void *p)
     return v;
 }
 
+// Bytes of (a, b) picked by the low four nibbles of s, whose top bits have to be zero (the intrinsic masks them off, one more
+// instruction each time).
+__device__ __forceinline__ uint32_t pick_bytes(uint32_t a, uint32_t b, uint32_t s)
+{
+    uint32_t r;
+    asm("prmt.b32 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(s));
+    return r;
+}
+
+__device__ __forceinline__ uint4 ld_shared_16(uint32_t addr)
+{
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+
 // The levels of a channel as byte planes.
 struct LevelPlanes {
     uint32_t lo[4], hi[4];
@@ -59,14 +75,14 @@ struct LevelPlanes {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const uint32_t s = h ? sel >> 16 : sel;
-            uint32_t l = __byte_perm(lo[0], lo[1], s), u = __byte_perm(hi[0], hi[1], s);
+            uint32_t l = pick_bytes(lo[0], lo[1], s), u = pick_bytes(hi[0], hi[1], s);
             if (WIDE) {
                 const uint32_t t = h ? top >> 16 : top;
-                l = __byte_perm(l, __byte_perm(lo[2], lo[3], s), t);
-                u = __byte_perm(u, __byte_perm(hi[2], hi[3], s), t);
+                l = pick_bytes(l, pick_bytes(lo[2], lo[3], s), t);
+                u = pick_bytes(u, pick_bytes(hi[2], hi[3], s), t);
             }
-            o[2 * h] = __byte_perm(l, u, 0x5140);
-            o[2 * h + 1] = __byte_perm(l, u, 0x7362);
+            o[2 * h] = pick_bytes(l, u, 0x5140);
+            o[2 * h + 1] = pick_bytes(l, u, 0x7362);
         }
         return out;
     }
@@ -79,14 +95,15 @@ __device__ __forceinline__ float activate(float z, int act)
     if (act == LIN_GELU) return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
     return z;
 }
+// The slope's fp32 value decides how dZ is rounded, and the fp32 gradients are those of the rounded dZ: no fast approximations.
 __device__ __forceinline__ float activation_slope(float z, int act)
 {
     if (act == LIN_RELU) return z > 0.0f ? 1.0f : 0.0f;
     if (act == LIN_SILU) {
-        const float sig = __fdividef(1.0f, 1.0f + __expf(-z));
+        const float sig = 1.0f / (1.0f + expf(-z));
         return sig * (1.0f + z * (1.0f - sig));
     }
-    if (act == LIN_GELU) return 0.5f * (1.0f + erff(z * 0.70710678118654752f)) + z * __expf(-0.5f * z * z) * 0.39894228040143268f;
+    if (act == LIN_GELU) return 0.5f * (1.0f + erff(z * 0.70710678118654752f)) + z * expf(-0.5f * z * z) * 0.39894228040143268f;
     return 1.0f;
 }
 
@@ -166,6 +183,7 @@ constexpr int LT_CHANNELS = 16;
 constexpr int LT_TOKENS = 8;
 constexpr int LT_K = 128;                 // contraction indices a warp takes at a time: 32 per lane of a quad
 constexpr int LT_MAX_CLUSTER = 8;
+constexpr int LT_AHEAD = 4;               // even
 
 template <bool BF16>
 __device__ __forceinline__ void mma_m16n8k16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
@@ -210,36 +228,50 @@ __global__ void __launch_bounds__(LT_THREADS) linear_token_kernel(const LinearPa
     const bool have = g < p.n;
     float c0[4] = {0.f, 0.f, 0.f, 0.f}, c1[4] = {0.f, 0.f, 0.f, 0.f};
     const int pieces = (p.d_in + LT_K - 1) / LT_K, stride = ranks * LT_WARPS;
-    struct Piece {
-        uint4 a, b, x[4];
+    struct Codes {
+        uint4 a, b;
     };
-    auto fetch = [&](int piece, Piece &f) {
+    struct Tokens {
+        uint4 x[4];
+    };
+    auto fetch_codes = [&](int piece, Codes &f) {
         const int k = piece * LT_K + 32 * t;
         const bool in = piece < pieces && k < p.d_in;
         f.a = in ? ld_once_16(reinterpret_cast<const uint4 *>(ca + (k >> 1))) : make_uint4(0u, 0u, 0u, 0u);
         f.b = in ? ld_once_16(reinterpret_cast<const uint4 *>(cb + (k >> 1))) : make_uint4(0u, 0u, 0u, 0u);
+    };
+    auto fetch_tokens = [&](int piece, Tokens &f) {
+        const int k = piece * LT_K + 32 * t;
 #pragma unroll
         for (int q = 0; q < 4; ++q)
-            f.x[q] = (in && have && k + 8 * q < p.d_in) ? ld_u32x4(x + k + 8 * q) : make_uint4(0u, 0u, 0u, 0u);
+            f.x[q] = (piece < pieces && have && k + 8 * q < p.d_in) ? ld_u32x4(x + k + 8 * q) : make_uint4(0u, 0u, 0u, 0u);
     };
-    auto use = [&](int piece, const Piece &f) {
+    auto use = [&](int piece, const Codes &f, const Tokens &y) {
         const uint32_t qa[4] = {f.a.x, f.a.y, f.a.z, f.a.w}, qb[4] = {f.b.x, f.b.y, f.b.z, f.b.w};
         const bool ragged = (piece + 1) * LT_K > p.d_in;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             uint4 wa = la.look<WIDE>(qa[q]), wb = lb.look<WIDE>(qb[q]);
             if (ragged && piece * LT_K + 32 * t + 8 * q >= p.d_in) wa = wb = make_uint4(0u, 0u, 0u, 0u);      // no level meets padding
-            mma_m16n8k16<BF16>(c0, wa.x, wb.x, wa.y, wb.y, f.x[q].x, f.x[q].y);
-            mma_m16n8k16<BF16>(c1, wa.z, wb.z, wa.w, wb.w, f.x[q].z, f.x[q].w);
+            mma_m16n8k16<BF16>(c0, wa.x, wb.x, wa.y, wb.y, y.x[q].x, y.x[q].y);
+            mma_m16n8k16<BF16>(c1, wa.z, wb.z, wa.w, wb.w, y.x[q].z, y.x[q].w);
         }
     };
+    // Codes are asked for LT_AHEAD pieces ahead (they come from device memory), activations one piece ahead (from L2 or L1).
     int piece = rank * LT_WARPS + warp;
-    Piece cur, next;
-    fetch(piece, cur);
-    for (; piece < pieces; piece += stride) {
-        fetch(piece + stride, next);
-        use(piece, cur);
-        cur = next;
+    Codes codes[LT_AHEAD];
+    Tokens tokens[2];
+#pragma unroll
+    for (int d = 0; d < LT_AHEAD; ++d) fetch_codes(piece + d * stride, codes[d]);
+    fetch_tokens(piece, tokens[0]);
+    while (piece < pieces) {
+#pragma unroll
+        for (int d = 0; d < LT_AHEAD; ++d) {
+            fetch_tokens(piece + stride, tokens[(d + 1) & 1]);
+            use(piece, codes[d], tokens[d & 1]);                  // nothing but zeros past the end
+            fetch_codes(piece + LT_AHEAD * stride, codes[d]);
+            piece += stride;
+        }
     }
     // c[0], c[1]: channel g, tokens 2 t, 2 t + 1; c[2], c[3]: channel g + 8
 #pragma unroll
@@ -272,13 +304,16 @@ __global__ void __launch_bounds__(LT_THREADS) linear_token_kernel(const LinearPa
 // ------------------------------------------------------------------------------------------------ tensor cores
 constexpr int LP_STAGES = 6;
 constexpr int LP_SLOT_BYTES = (CTA_ROWS / BOX_FEATURES) * BOX_BYTES;      // one operand block: 16 KB
-constexpr int LP_STAGE_BYTES = 2 * LP_SLOT_BYTES;                         // [weights | tokens]
-constexpr int LP_LOOK_WARPS = 8;                                          // two groups of four, every other k-step each
+constexpr int LP_CODE_BYTES = CTA_ROWS * TILE_K / 2;                      // codes of an operand block: 4 KB
+constexpr int LP_STAGE_BYTES = 2 * LP_SLOT_BYTES + LP_CODE_BYTES;         // [weights | tokens | codes]
+constexpr int LP_LOOK_GROUPS = 2;                                         // of four warps; they take the k-steps in turn
+constexpr int LP_LOOK_WARPS = 4 * LP_LOOK_GROUPS;
 constexpr int LP_EPI_WARPS = 8;
 constexpr int LP_THREADS = 32 * (4 + LP_LOOK_WARPS + LP_EPI_WARPS);
 constexpr int LP_SMEM_BYTES = LP_STAGES * LP_STAGE_BYTES + 1024;
-constexpr int LG_STAGES = 6;                                              // gradient of the levels: [dZ | tokens]
-constexpr int LG_SMEM_BYTES = LG_STAGES * LP_STAGE_BYTES + LP_EPI_WARPS * LIN_LEVELS * 32 * 4 + 1024;
+constexpr int LG_STAGES = 6;                                              // gradient of the levels
+constexpr int LG_STAGE_BYTES = 2 * LP_SLOT_BYTES;                         // [dZ | tokens]
+constexpr int LG_SMEM_BYTES = LG_STAGES * LG_STAGE_BYTES + LP_EPI_WARPS * LIN_LEVELS * 32 * 4 + 1024;
 constexpr int LG_THREADS = 32 * (4 + LP_EPI_WARPS);
 constexpr int LG_CHUNK_KSTEPS = 16;                                       // 1024 tokens
 constexpr int LP_ROW_BLOCK = 16;                                          // row tiles that are worked on beside each other
@@ -321,14 +356,16 @@ __device__ __forceinline__ bool linear_unit(const LinearParams &p, int pair, int
 
 // Forward (BACK false): D[channel][token] = sum_c W[channel][c] X[token][c], both operands with the contraction contiguous; a lookup thread
 // owns a channel for the whole tile, its levels stay in registers.  Backward: D[c][token] = sum_j W[j][c] dZ[token][j]; the rows of
-// the weight operand are contraction indices, a lookup thread owns 64 columns of one channel a k-step and fetches that
-// channel's levels with the codes.  The codes of a thread's next k-step are read while it looks the present ones up.
+// the weight operand are contraction indices, a lookup thread owns 64 columns of one channel a k-step and reads that channel's levels
+// a step ahead.  Codes come by TMA as well, into the stage they will fill: read by the lookup threads from global memory, 32 bytes
+// of a row each, they cost 28 us of 313 (8192 x 4096 x 4096).
 // Rows of D are the lanes of tensor memory, so tokens (columns) come in any number without work for the weights' side.
 template <bool BACK, bool WIDE>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LP_THREADS, 1)
-linear_pair_kernel(const __grid_constant__ CUtensorMap mapX, const LinearParams p)
+linear_pair_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_constant__ CUtensorMap mapC, const LinearParams p)
 {
     extern __shared__ uint8_t smem_raw[];
+    __shared__ __align__(8) uint64_t bar_codes[LP_STAGES];    // this CTA's codes
     __shared__ __align__(8) uint64_t bar_full[LP_STAGES];     // first CTA: bytes of both CTAs + four lookup warps of both
     __shared__ __align__(8) uint64_t bar_empty[LP_STAGES];    // both CTAs: signalled by the MMA commits
     __shared__ __align__(8) uint64_t bar_acc_full[2];         // both CTAs, one per accumulator
@@ -347,7 +384,8 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap mapX, const LinearParams 
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < LP_STAGES; ++s) {
-            mbar_init(smem_u32(&bar_full[s]), 1 + LP_LOOK_WARPS);
+            mbar_init(smem_u32(&bar_codes[s]), 1);
+            mbar_init(smem_u32(&bar_full[s]), 1 + 2 * 4);
             mbar_init(smem_u32(&bar_empty[s]), 1);
         }
         for (int b = 0; b < 2; ++b) {
@@ -358,6 +396,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap mapX, const LinearParams 
         abort_flag = 0u;
         fence_mbar_init();
         prefetch_tensormap(&mapX);
+        prefetch_tensormap(&mapC);
     }
     griddep_launch();
     if (warp == 2) {
@@ -372,20 +411,22 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap mapX, const LinearParams 
     griddep_wait();
 
     if (warp == 0 && lane == 0) {
-        // ------------------------------------------------------------------ TMA producer (both CTAs): tokens
+        // ------------------------------------------------------------------ TMA producer (both CTAs): codes and tokens
         int s = 0;
         uint32_t ph = 0;
         uint32_t issued = 0;
         bool ok = true;
         LinearUnit u;
         for (int it = 0; ok && linear_unit(p, pair, it, u); ++it) {
-            const int b0 = u.tok0 + static_cast<int>(rank) * CTA_ROWS;
+            const int a0 = u.row0 + static_cast<int>(rank) * CTA_ROWS, b0 = u.tok0 + static_cast<int>(rank) * CTA_ROWS;
             for (int kb = 0; kb < kblocks; ++kb) {
                 if (!bounded_wait(smem_u32(&bar_empty[s]), ph ^ 1u, wc, 1u, it)) { ok = false; break; }
                 const uint32_t full_local = smem_u32(&bar_full[s]);
                 if (rank == 0) mbar_arrive_expect_tx(full_local, 2 * LP_SLOT_BYTES);      // both CTAs' bytes
                 const uint32_t full = map_to_cta(full_local, 0);
                 const uint32_t stage = ring + s * LP_STAGE_BYTES;
+                mbar_arrive_expect_tx(smem_u32(&bar_codes[s]), LP_CODE_BYTES);
+                tma_load_3d(stage + 2 * LP_SLOT_BYTES, &mapC, smem_u32(&bar_codes[s]), (BACK ? a0 : kb * TILE_K) >> 1, BACK ? kb * TILE_K : a0, 0);
 #pragma unroll
                 for (int q = 0; q < CTA_ROWS / TILE_K; ++q)
                     tma_load_3d_pair(stage + LP_SLOT_BYTES + q * BOX_BYTES, &mapX, full, kb * TILE_K, b0 + q * TILE_K, 0);
@@ -440,88 +481,74 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap mapX, const LinearParams 
         }
     } else if (warp >= 4 && warp < 4 + LP_LOOK_WARPS) {
         // ------------------------------------------------------------------ weight operand
-        const int grp = (warp - 4) >> 2;                            // takes k-steps grp, grp + 2, ... of the launch
+        const int grp = (warp - 4) >> 2;                            // takes k-steps grp, grp + LP_LOOK_GROUPS, ... of the launch
         const int r = ((warp - 4) & 3) * 32 + lane;                 // forward: channel; backward: channel r % 64, columns 64 (r / 64) ..
         const uint32_t slot = BACK ? static_cast<uint32_t>((r >> 6) * BOX_BYTES + (r & 63) * 128) : static_cast<uint32_t>(r * 128);
+        const uint32_t code_at = 2 * LP_SLOT_BYTES + (BACK ? static_cast<uint32_t>((r & 63) * 64 + (r >> 6) * 32) : static_cast<uint32_t>(r * 32));
         const uint32_t xor7 = static_cast<uint32_t>(r & 7);
-        struct Fetch {
-            uint4 c[2], t[2];
+        // Backward: the levels of channel r % 64 of k-step kb, asked for a k-step of the group ahead.
+        struct Levels {
+            uint4 a, b;
         };
-        auto fetch = [&](const LinearUnit &u, int kb, Fetch &f) {
-            const int row = u.row0 + static_cast<int>(rank) * CTA_ROWS + (BACK ? (r >> 6) * 64 : r);
-            const int j = BACK ? kb * TILE_K + (r & 63) : row;
-            const int byte = (BACK ? row : kb * TILE_K) >> 1;
-            const bool in = j < p.d_out;
-            const uint8_t *at = p.codes + static_cast<size_t>(in ? j : 0) * p.ld_codes + byte;
-#pragma unroll
-            for (int q = 0; q < 2; ++q)
-                f.c[q] = (in && byte + 16 * q < p.ld_codes) ? ld_u32x4(at + 16 * q) : make_uint4(0u, 0u, 0u, 0u);
-            if (BACK) {
-                const uint4 *tb = reinterpret_cast<const uint4 *>(p.table + static_cast<size_t>(in ? j : 0) * LIN_LEVELS);
-#pragma unroll
-                for (int q = 0; q < 2; ++q) f.t[q] = in ? ld_u32x4(tb + q) : make_uint4(0u, 0u, 0u, 0u);
-            }
+        auto levels_at = [&](int j, Levels &t) {
+            const uint4 *tb = reinterpret_cast<const uint4 *>(p.table + static_cast<size_t>(j < p.d_out ? j : 0) * LIN_LEVELS);
+            t.a = ld_u32x4(tb);
+            t.b = ld_u32x4(tb + 1);
         };
         LevelPlanes lv;
         int s = grp;
         uint32_t ph = 0;
-        int kb = grp;                                               // next k-step of this group
+        int kb = grp, it = 0, levels_of = -1;
         bool ok = true;
-        LinearUnit u, un;
-        int it = 0;
+        LinearUnit u;
         bool valid = linear_unit(p, pair, 0, u);
-        while (valid && kb >= kblocks) {                            // kblocks may be 1
-            kb -= kblocks;
-            valid = linear_unit(p, pair, ++it, u);
-        }
-        Fetch cur, next;
-        if (valid) fetch(u, kb, cur);
-        bool fresh = true;                                          // a new tile: the channel's levels
+        auto settle = [&]() {                                       // into the tile that the k-step lies in
+            while (valid && kb >= kblocks) {
+                kb -= kblocks;
+                valid = linear_unit(p, pair, ++it, u);
+            }
+        };
+        settle();
+        Levels ahead{};
+        if (BACK && valid) levels_at(kb * TILE_K + (r & 63), ahead);
         while (valid) {
-            if (!BACK && fresh) {
-                const int j = u.row0 + static_cast<int>(rank) * CTA_ROWS + r;
-                const uint4 *tb = reinterpret_cast<const uint4 *>(p.table + static_cast<size_t>(j < p.d_out ? j : 0) * LIN_LEVELS);
-                const uint4 t0 = ld_u32x4(tb), t1 = ld_u32x4(tb + 1);
-                lv.set(t0, t1);
+            if (BACK) {
+                lv.set(ahead.a, ahead.b);
+                int kn = kb + LP_LOOK_GROUPS;                       // (past the last tile: some channel's levels, not used)
+                while (kn >= kblocks) kn -= kblocks;
+                levels_at(kn * TILE_K + (r & 63), ahead);
+            } else if (levels_of != it) {
+                levels_of = it;
+                levels_at(u.row0 + static_cast<int>(rank) * CTA_ROWS + r, ahead);
+                lv.set(ahead.a, ahead.b);
             }
-            // the k-step after this one
-            int kn = kb + 2, itn = it;
-            bool vn = true;
-            un = u;
-            while (vn && kn >= kblocks) {
-                kn -= kblocks;
-                vn = linear_unit(p, pair, ++itn, un);
-            }
-            if (vn) fetch(un, kn, next);
-            if (BACK) lv.set(cur.t[0], cur.t[1]);
+            // the codes are there: the stage has been released before
             bool got = true;
-            if (lane == 0) got = bounded_wait(smem_u32(&bar_empty[s]), ph ^ 1u, wc, 6u, it);
+            if (lane == 0) got = bounded_wait(smem_u32(&bar_codes[s]), ph, wc, 6u, it);
             got = __any_sync(0xffffffffu, got && lane == 0);
             if (!got) { ok = false; break; }
-            (void)mbar_try_wait(smem_u32(&bar_empty[s]), ph ^ 1u);           // every lane observes the completed phase
-            const uint32_t base = ring + s * LP_STAGE_BYTES + slot;
-            const bool ragged = !BACK && (kb + 1) * TILE_K > kdim;
+            (void)mbar_try_wait(smem_u32(&bar_codes[s]), ph);                // every lane observes the completed phase
+            const uint32_t stage = ring + s * LP_STAGE_BYTES, base = stage + slot;
+            // the last, ragged k-step: no level meets padding (infinite ones would make it NaN)
+            const int end = BACK ? p.d_out - (kb * TILE_K + (r & 63)) > 0 ? TILE_K : 0 : p.d_in - kb * TILE_K;
 #pragma unroll
             for (int q = 0; q < 2; ++q) {
-                const uint32_t w[4] = {cur.c[q].x, cur.c[q].y, cur.c[q].z, cur.c[q].w};
+                const uint4 c = ld_shared_16(stage + code_at + 16 * q);
+                const uint32_t w[4] = {c.x, c.y, c.z, c.w};
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     uint4 v = lv.look<WIDE>(w[e]);
-                    if (ragged && kb * TILE_K + 32 * q + 8 * e >= kdim) v = make_uint4(0u, 0u, 0u, 0u);      // no level meets padding
+                    if (32 * q + 8 * e >= end) v = make_uint4(0u, 0u, 0u, 0u);
                     st_shared_16(base + ((static_cast<uint32_t>(4 * q + e) ^ xor7) << 4), v);
                 }
             }
             fence_proxy_async_smem();                // make the stores visible to the tensor core's reads
             __syncwarp();
             if (lane == 0) mbar_arrive_cluster(map_to_cta(smem_u32(&bar_full[s]), 0));
-            s += 2;
+            s += LP_LOOK_GROUPS;
             if (s >= LP_STAGES) { s -= LP_STAGES; ph ^= 1u; }
-            fresh = itn != it;
-            kb = kn;
-            it = itn;
-            u = un;
-            valid = vn;
-            cur = next;
+            kb += LP_LOOK_GROUPS;
+            settle();
         }
         (void)ok;
     } else if (warp >= 4 + LP_LOOK_WARPS) {
@@ -530,11 +557,17 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap mapX, const LinearParams 
         const int q = warp & 3;                         // TMEM lane quarter this warp may access
         const int half = ew >> 2;                       // which 128 of the 256 tokens
         const bool bf16 = p.bf16 != 0;
+        // Lanes 2 i and 2 i + 1 exchange every other token, so that each holds two neighbouring rows of a token: 4-byte accesses.
+        const int odd = lane & 1;
         uint32_t full_ph = 0u;                          // bit b: phase of accumulator b
         int buf = 0;
         bool ok = true;
         LinearUnit u;
         for (int it = 0; ok && linear_unit(p, pair, it, u); ++it) {
+            const int row = u.row0 + static_cast<int>(rank) * CTA_ROWS + q * 32 + lane;
+            const bool in = row < rows;
+            float bias = 0.0f;
+            if (!BACK && p.bias && in) bias = half_value(ld_u16(p.bias + row), bf16);
             if (lane == 0) ok = bounded_wait(smem_u32(&bar_acc_full[buf]), (full_ph >> buf) & 1u, wc, 4u, it);
             ok = __shfl_sync(0xffffffffu, ok, 0);
             if (!ok) break;
@@ -542,12 +575,8 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap mapX, const LinearParams 
             full_ph ^= 1u << buf;
             tc_fence_after_sync();
             const uint32_t tmem_tile = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + static_cast<uint32_t>(buf * TILE_N + half * 128);
-            const int row = u.row0 + static_cast<int>(rank) * CTA_ROWS + q * 32 + lane;
-            const bool in = row < rows;
-            float bias = 0.0f;
-            if (!BACK && p.bias && in) bias = half_value(ld_u16(p.bias + row), bf16);
-            // Lanes 2 i and 2 i + 1 exchange every other token, so that each holds two neighbouring rows of a token: 4-byte accesses.
-            const int odd = lane & 1, pair_row = row - odd;
+            // even lane: tokens 0, 2, ... of rows (row, row + 1); odd lane: tokens 1, 3, ... of rows (row - 1, row)
+            const long long tok0 = u.tok0 + half * 128 + odd;
 #pragma unroll 1
             for (int n0 = 0; n0 < 128; n0 += 32) {
                 uint32_t acc[32];
@@ -558,29 +587,50 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap mapX, const LinearParams 
                     __syncwarp();
                     if (lane == 0) mbar_arrive_cluster(map_to_cta(smem_u32(&bar_acc_empty[buf]), 0));
                 }
-                const int tok0 = u.tok0 + half * 128 + n0;
-                if (tok0 >= p.n) continue;
+                const int left = in ? p.n - static_cast<int>(tok0) - n0 : 0;       // this lane's tokens 0, 2, ... below it exist
+                float2 v[16];
 #pragma unroll
-                for (int e = 0; e < 32; e += 2) {
-                    float v0 = __uint_as_float(acc[e]) + bias, v1 = __uint_as_float(acc[e + 1]) + bias;
-                    const float other = __shfl_xor_sync(0xffffffffu, odd ? v0 : v1, 1);
-                    if (odd) v0 = other;
-                    else v1 = other;
-                    // even lane: token e of rows (row, row + 1); odd lane: token e + 1 of rows (row - 1, row)
-                    const int token = tok0 + e + odd;
-                    if (in && token < p.n) {
-                        if (!BACK) {
-                            if (p.Z) *reinterpret_cast<uint32_t *>(p.Z + token * p.ld_z + pair_row) = half2_bits(v0, v1, bf16);
-                            v0 = activate(v0, p.act);
-                            v1 = activate(v1, p.act);
-                            if (p.residual) {
-                                const float2 res = half2_value(*reinterpret_cast<const uint32_t *>(p.residual + token * p.ld_r + pair_row), bf16);
-                                v0 += res.x;
-                                v1 += res.y;
-                            }
+                for (int e = 0; e < 16; ++e) {
+                    const float a = __uint_as_float(acc[2 * e]) + bias, b = __uint_as_float(acc[2 * e + 1]) + bias;
+                    const float other = __shfl_xor_sync(0xffffffffu, odd ? a : b, 1);
+                    v[e] = odd ? make_float2(other, b) : make_float2(a, other);
+                }
+                if (!BACK) {
+                    if (p.Z) {
+                        uint16_t *z = p.Z + (tok0 + n0) * p.ld_z + (row - odd);
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            if (2 * e < left) *reinterpret_cast<uint32_t *>(z) = half2_bits(v[e].x, v[e].y, bf16);
+                            z += 2 * p.ld_z;
                         }
-                        *reinterpret_cast<uint32_t *>(p.out + token * p.ld_out + pair_row) = half2_bits(v0, v1, bf16);
                     }
+                    uint32_t res[16];
+                    if (p.residual) {
+                        const uint16_t *at = p.residual + (tok0 + n0) * p.ld_r + (row - odd);
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            res[e] = 2 * e < left ? *reinterpret_cast<const uint32_t *>(at) : 0u;
+                            at += 2 * p.ld_r;
+                        }
+                    }
+                    if (p.act != LIN_NONE) {
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) v[e] = make_float2(activate(v[e].x, p.act), activate(v[e].y, p.act));
+                    }
+                    if (p.residual) {
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            const float2 t = half2_value(res[e], bf16);
+                            v[e].x += t.x;
+                            v[e].y += t.y;
+                        }
+                    }
+                }
+                uint16_t *out = p.out + (tok0 + n0) * p.ld_out + (row - odd);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    if (2 * e < left) *reinterpret_cast<uint32_t *>(out) = half2_bits(v[e].x, v[e].y, bf16);
+                    out += 2 * p.ld_out;
                 }
             }
             buf ^= 1;
@@ -767,7 +817,7 @@ linear_level_grad_kernel(const __grid_constant__ CUtensorMap mapG, const __grid_
                 const uint32_t full_local = smem_u32(&bar_full[s]);
                 if (rank == 0) mbar_arrive_expect_tx(full_local, 4 * LP_SLOT_BYTES);      // both CTAs' bytes
                 const uint32_t full = map_to_cta(full_local, 0);
-                const uint32_t stage = ring + s * LP_STAGE_BYTES;
+                const uint32_t stage = ring + s * LG_STAGE_BYTES;
 #pragma unroll
                 for (int q = 0; q < CTA_ROWS / BOX_FEATURES; ++q) {
                     tma_load_3d_pair(stage + q * BOX_BYTES, &mapG, full, a0 + q * BOX_FEATURES, kb * TILE_K, 0);
@@ -800,7 +850,7 @@ linear_level_grad_kernel(const __grid_constant__ CUtensorMap mapG, const __grid_
             for (int kb = u.t0; kb < u.t1; ++kb) {
                 if (!bounded_wait_hot(smem_u32(&bar_full[s]), ph, wc, 3u, u.tile)) { ok = false; break; }
                 tc_fence_after_sync();
-                const uint32_t sa = ring + s * LP_STAGE_BYTES;
+                const uint32_t sa = ring + s * LG_STAGE_BYTES;
                 const uint32_t sb = sa + LP_SLOT_BYTES;
 #pragma unroll
                 for (int k16 = 0; k16 < TILE_K / 16; ++k16) {
@@ -827,7 +877,7 @@ linear_level_grad_kernel(const __grid_constant__ CUtensorMap mapG, const __grid_
         const int ew = warp - 4;                        // 0..7; four consecutive warps cover the four lane quarters
         const int q = warp & 3;                         // TMEM lane quarter this warp may access
         const int half = ew >> 2;                       // which 128 of the 256 features
-        float *sums = reinterpret_cast<float *>(smem_raw + (ring - smem_u32(smem_raw)) + LG_STAGES * LP_STAGE_BYTES) + ew * LIN_LEVELS * 32 + lane;
+        float *sums = reinterpret_cast<float *>(smem_raw + (ring - smem_u32(smem_raw)) + LG_STAGES * LG_STAGE_BYTES) + ew * LIN_LEVELS * 32 + lane;
 #pragma unroll
         for (int l = 0; l < LIN_LEVELS; ++l) sums[l * 32] = 0.0f;
         uint32_t full_ph = 0u;                          // bit b: phase of accumulator b
