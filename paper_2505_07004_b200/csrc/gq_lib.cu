@@ -1484,11 +1484,15 @@ static CUtensorMapDataType map_type(int32_t dtype)
 static int32_t linear_pair(bool back, gq::LinearParams p, int32_t dtype, const void *in, int64_t ld_in, int32_t m, DeviceInfo *di, cudaStream_t st)
 {
     const int rows = back ? p.d_in : p.d_out, kdim = back ? p.d_out : p.d_in;
-    const int64_t row_tiles = (rows + gq::TILE_M - 1) / gq::TILE_M, tok_tiles = (p.n + gq::TILE_N - 1) / gq::TILE_N;
-    if (row_tiles * tok_tiles >= (1ll << 30)) return GQ_ERR_UNSUPPORTED_SHAPE;
+    const int64_t row_tiles = (rows + gq::TILE_M - 1) / gq::TILE_M;
+    const int64_t tok_tiles = (p.n + gq::LP_HALVES * gq::TILE_N - 1) / (gq::LP_HALVES * gq::TILE_N), tiles = row_tiles * tok_tiles;
+    if (tiles >= (1ll << 29)) return GQ_ERR_UNSUPPORTED_SHAPE;
     p.row_tiles = static_cast<int>(row_tiles);
     p.tok_tiles = static_cast<int>(tok_tiles);
-    p.units = static_cast<int>(row_tiles * tok_tiles);
+    // Whole tiles (two halves on one looked-up operand) in full rounds; the last round as halves where there are pairs for all of them.
+    const int rest = static_cast<int>(tiles % di->max_pairs);
+    p.doubles = static_cast<int>(2 * rest <= di->max_pairs && p.n > gq::TILE_N ? tiles - rest : tiles);
+    p.units = p.doubles + 2 * (static_cast<int>(tiles) - p.doubles);
     p.pairs = p.units < di->max_pairs ? p.units : di->max_pairs;
     p.status = di->status_ptr;
     p.wait_budget_ns = wait_budget_ns();

@@ -172,7 +172,7 @@ struct LinearParams {
     const uint16_t *X;       // few tokens only: the pair kernel reads X through a tensor map
     long long ld_x;
     // pair kernel
-    int row_tiles, tok_tiles, units, pairs;
+    int row_tiles, tok_tiles, doubles, units, pairs;      // tiles of 256 rows, of 512 tokens
     uint32_t *status;
     unsigned long long wait_budget_ns;
 };
@@ -302,15 +302,17 @@ __global__ void __launch_bounds__(LT_THREADS) linear_token_kernel(const LinearPa
 }
 
 // ------------------------------------------------------------------------------------------------ tensor cores
-constexpr int LP_STAGES = 6;
 constexpr int LP_SLOT_BYTES = (CTA_ROWS / BOX_FEATURES) * BOX_BYTES;      // one operand block: 16 KB
+constexpr int LP_HALVES = 2;                                              // token tiles of 256 that share a weight operand
+constexpr int LP_STAGES = 4;
+constexpr int LP_STAGE_BYTES = (1 + LP_HALVES) * LP_SLOT_BYTES;           // [weights | tokens | tokens]
 constexpr int LP_CODE_BYTES = CTA_ROWS * TILE_K / 2;                      // codes of an operand block: 4 KB
-constexpr int LP_STAGE_BYTES = 2 * LP_SLOT_BYTES + LP_CODE_BYTES;         // [weights | tokens | codes]
+constexpr int LP_CODE_SLOTS = 8;
 constexpr int LP_LOOK_GROUPS = 2;                                         // of four warps; they take the k-steps in turn
 constexpr int LP_LOOK_WARPS = 4 * LP_LOOK_GROUPS;
 constexpr int LP_EPI_WARPS = 8;
 constexpr int LP_THREADS = 32 * (4 + LP_LOOK_WARPS + LP_EPI_WARPS);
-constexpr int LP_SMEM_BYTES = LP_STAGES * LP_STAGE_BYTES + 1024;
+constexpr int LP_SMEM_BYTES = LP_STAGES * LP_STAGE_BYTES + LP_CODE_SLOTS * LP_CODE_BYTES + 1024;
 constexpr int LG_STAGES = 6;                                              // gradient of the levels
 constexpr int LG_STAGE_BYTES = 2 * LP_SLOT_BYTES;                         // [dZ | tokens]
 constexpr int LG_SMEM_BYTES = LG_STAGES * LG_STAGE_BYTES + LP_EPI_WARPS * LIN_LEVELS * 32 * 4 + 1024;
@@ -338,34 +340,44 @@ __host__ __device__ constexpr uint32_t umma_idesc_16(uint32_t m, uint32_t n, boo
 }
 
 struct LinearUnit {
-    int row0, tok0;
+    int row0, tok0, halves;      // 256 rows of the weights' side, `halves` tiles of 256 tokens from tok0 on
 };
-// The it-th tile of a pair.  Row tiles in blocks of LP_ROW_BLOCK, inside a block token tiles outermost: tiles worked on at the same time
-// share few token tiles (2 bytes an element) and more row tiles (half a byte).
+// The it-th unit of a pair.  Tiles of 256 rows x 512 tokens: the first `doubles` of them whole, the others in two units.  Row tiles in
+// blocks of LP_ROW_BLOCK, inside a block token tiles outermost: tiles worked on at the same time share few token tiles (2 bytes an
+// element) and more row tiles (half a byte).
 __device__ __forceinline__ bool linear_unit(const LinearParams &p, int pair, int it, LinearUnit &u)
 {
     const int unit = it * p.pairs + pair;
     if (unit >= p.units) return false;
-    const int per = LP_ROW_BLOCK * p.tok_tiles, block = unit / per, rest = unit - block * per;
+    const int over = unit - p.doubles, tile = over < 0 ? unit : p.doubles + (over >> 1);
+    const int per = LP_ROW_BLOCK * p.tok_tiles, block = tile / per, rest = tile - block * per;
     const int left = p.row_tiles - block * LP_ROW_BLOCK, width = left < LP_ROW_BLOCK ? left : LP_ROW_BLOCK;
     const int tok = rest / width;
     u.row0 = (block * LP_ROW_BLOCK + rest - tok * width) * TILE_M;
-    u.tok0 = tok * TILE_N;
+    u.tok0 = tok * (LP_HALVES * TILE_N);
+    u.halves = u.tok0 + TILE_N < p.n ? 2 : 1;
+    if (over >= 0) {
+        // (the second unit of a tile without a second half has nothing to do)
+        if ((over & 1) != 0 && u.halves == 2) u.tok0 += TILE_N;
+        u.halves = (over & 1) != 0 && u.halves == 1 ? 0 : 1;
+    }
     return true;
 }
 
 // Forward (BACK false): D[channel][token] = sum_c W[channel][c] X[token][c], both operands with the contraction contiguous; a lookup thread
 // owns a channel for the whole tile, its levels stay in registers.  Backward: D[c][token] = sum_j W[j][c] dZ[token][j]; the rows of
 // the weight operand are contraction indices, a lookup thread owns 64 columns of one channel a k-step and reads that channel's levels
-// a step ahead.  Codes come by TMA as well, into the stage they will fill: read by the lookup threads from global memory, 32 bytes
-// of a row each, they cost 28 us of 313 (8192 x 4096 x 4096).
+// a step ahead.  Codes come by TMA as well: read by the lookup threads from global memory, 32 bytes of a row each, they cost
+// 28 us of 313 (8192 x 4096 x 4096).  A looked-up operand serves two tiles of 256 tokens, the two accumulators that tensor memory
+// holds: with one tile each, lookups and their stores were in the way of the tensor core (263 us, 221 with the lookups left out).
 // Rows of D are the lanes of tensor memory, so tokens (columns) come in any number without work for the weights' side.
 template <bool BACK, bool WIDE>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LP_THREADS, 1)
 linear_pair_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_constant__ CUtensorMap mapC, const LinearParams p)
 {
     extern __shared__ uint8_t smem_raw[];
-    __shared__ __align__(8) uint64_t bar_codes[LP_STAGES];    // this CTA's codes
+    __shared__ __align__(8) uint64_t bar_codes[LP_CODE_SLOTS];       // this CTA's codes have come
+    __shared__ __align__(8) uint64_t bar_codes_used[LP_CODE_SLOTS];  // four lookup warps have read them
     __shared__ __align__(8) uint64_t bar_full[LP_STAGES];     // first CTA: bytes of both CTAs + four lookup warps of both
     __shared__ __align__(8) uint64_t bar_empty[LP_STAGES];    // both CTAs: signalled by the MMA commits
     __shared__ __align__(8) uint64_t bar_acc_full[2];         // both CTAs, one per accumulator
@@ -378,13 +390,16 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_consta
     const int lane = threadIdx.x & 31;
     const uint32_t rank = cluster_ctarank();
     const int pair = static_cast<int>(blockIdx.x >> 1);
-    const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u, code_ring = ring + LP_STAGES * LP_STAGE_BYTES;
     const int kdim = BACK ? p.d_out : p.d_in, rows = BACK ? p.d_in : p.d_out;
     const int kblocks = (kdim + TILE_K - 1) / TILE_K;
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < LP_STAGES; ++s) {
+        for (int s = 0; s < LP_CODE_SLOTS; ++s) {
             mbar_init(smem_u32(&bar_codes[s]), 1);
+            mbar_init(smem_u32(&bar_codes_used[s]), 4);
+        }
+        for (int s = 0; s < LP_STAGES; ++s) {
             mbar_init(smem_u32(&bar_full[s]), 1 + 2 * 4);
             mbar_init(smem_u32(&bar_empty[s]), 1);
         }
@@ -411,25 +426,25 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_consta
     griddep_wait();
 
     if (warp == 0 && lane == 0) {
-        // ------------------------------------------------------------------ TMA producer (both CTAs): codes and tokens
+        // ------------------------------------------------------------------ TMA producer (both CTAs): tokens
         int s = 0;
         uint32_t ph = 0;
         uint32_t issued = 0;
         bool ok = true;
         LinearUnit u;
         for (int it = 0; ok && linear_unit(p, pair, it, u); ++it) {
-            const int a0 = u.row0 + static_cast<int>(rank) * CTA_ROWS, b0 = u.tok0 + static_cast<int>(rank) * CTA_ROWS;
+            if (u.halves == 0) continue;
+            const int b0 = u.tok0 + static_cast<int>(rank) * CTA_ROWS;
             for (int kb = 0; kb < kblocks; ++kb) {
                 if (!bounded_wait(smem_u32(&bar_empty[s]), ph ^ 1u, wc, 1u, it)) { ok = false; break; }
                 const uint32_t full_local = smem_u32(&bar_full[s]);
-                if (rank == 0) mbar_arrive_expect_tx(full_local, 2 * LP_SLOT_BYTES);      // both CTAs' bytes
+                if (rank == 0) mbar_arrive_expect_tx(full_local, 2 * u.halves * LP_SLOT_BYTES);      // both CTAs' bytes
                 const uint32_t full = map_to_cta(full_local, 0);
                 const uint32_t stage = ring + s * LP_STAGE_BYTES;
-                mbar_arrive_expect_tx(smem_u32(&bar_codes[s]), LP_CODE_BYTES);
-                tma_load_3d(stage + 2 * LP_SLOT_BYTES, &mapC, smem_u32(&bar_codes[s]), (BACK ? a0 : kb * TILE_K) >> 1, BACK ? kb * TILE_K : a0, 0);
+                for (int h = 0; h < u.halves; ++h)
 #pragma unroll
-                for (int q = 0; q < CTA_ROWS / TILE_K; ++q)
-                    tma_load_3d_pair(stage + LP_SLOT_BYTES + q * BOX_BYTES, &mapX, full, kb * TILE_K, b0 + q * TILE_K, 0);
+                    for (int q = 0; q < CTA_ROWS / TILE_K; ++q)
+                        tma_load_3d_pair(stage + (1 + h) * LP_SLOT_BYTES + q * BOX_BYTES, &mapX, full, kb * TILE_K, b0 + h * TILE_N + q * TILE_K, 0);
                 ++issued;
                 if (++s == LP_STAGES) { s = 0; ph ^= 1u; }
             }
@@ -441,37 +456,80 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_consta
             if (++s == LP_STAGES) { s = 0; ph ^= 1u; }
         }
         if (!ok) spin_ns(1000000ull);
+    } else if (warp == 1 && lane == 0) {
+        // ------------------------------------------------------------------ TMA producer (both CTAs): codes
+        int c = 0;
+        uint32_t ph = 0;
+        bool ok = true;
+        LinearUnit u;
+        for (int it = 0; ok && linear_unit(p, pair, it, u); ++it) {
+            if (u.halves == 0) continue;
+            const int a0 = u.row0 + static_cast<int>(rank) * CTA_ROWS;
+            for (int kb = 0; kb < kblocks; ++kb) {
+                if (!bounded_wait(smem_u32(&bar_codes_used[c]), ph ^ 1u, wc, 7u, it)) { ok = false; break; }
+                const uint32_t bar = smem_u32(&bar_codes[c]);
+                mbar_arrive_expect_tx(bar, LP_CODE_BYTES);
+                tma_load_3d(code_ring + c * LP_CODE_BYTES, &mapC, bar, (BACK ? a0 : kb * TILE_K) >> 1, BACK ? kb * TILE_K : a0, 0);
+                if (++c == LP_CODE_SLOTS) { c = 0; ph ^= 1u; }
+            }
+        }
+        if (!ok) spin_ns(1000000ull);
     } else if (warp == 3 && lane == 0 && rank == 0) {
         // ------------------------------------------------------------------ MMA issuer (first CTA)
         const uint32_t idesc = umma_idesc_16(TILE_M, TILE_N, p.bf16 != 0, BACK, false);
         int s = 0;
         uint32_t ph = 0;
         uint32_t acc_ph = 0u;                           // bit b: phase of accumulator b
-        int buf = 0;
+        int buf = 0;                                    // accumulator of a unit's first half
         bool ok = true;
+        auto multiply = [&](int stage, int half, uint32_t d_tmem, bool first) {
+            const uint32_t sa = ring + stage * LP_STAGE_BYTES, sb = sa + (1 + half) * LP_SLOT_BYTES;
+#pragma unroll
+            for (int k16 = 0; k16 < TILE_K / 16; ++k16) {
+                const uint64_t adesc = BACK ? umma_smem_desc_mn_sw128(sa + k16 * 16 * 128, BOX_BYTES, 1024) : umma_smem_desc_k_sw128(sa + k16 * 32);
+                const uint64_t bdesc = umma_smem_desc_k_sw128(sb + k16 * 32);
+                umma_bf16(d_tmem, adesc, bdesc, idesc, (!first || k16 != 0) ? 1u : 0u);
+            }
+        };
+        auto acquire = [&](int b, int it) {
+            if (!bounded_wait_hot(smem_u32(&bar_acc_empty[b]), ((acc_ph >> b) & 1u) ^ 1u, wc, 2u, it)) return false;
+            acc_ph ^= 1u << b;
+            tc_fence_after_sync();
+            return true;
+        };
         LinearUnit u;
         for (int it = 0; ok && linear_unit(p, pair, it, u); ++it) {
-            if (!bounded_wait_hot(smem_u32(&bar_acc_empty[buf]), ((acc_ph >> buf) & 1u) ^ 1u, wc, 2u, it)) { ok = false; break; }
-            tc_fence_after_sync();
-            const uint32_t d_tmem = tmem_base + static_cast<uint32_t>(buf * TILE_N);
-            for (int kb = 0; kb < kblocks; ++kb) {
-                if (!bounded_wait_hot(smem_u32(&bar_full[s]), ph, wc, 3u, it)) { ok = false; break; }
-                tc_fence_after_sync();
-                const uint32_t sa = ring + s * LP_STAGE_BYTES;
-                const uint32_t sb = sa + LP_SLOT_BYTES;
-#pragma unroll
-                for (int k16 = 0; k16 < TILE_K / 16; ++k16) {
-                    const uint64_t adesc = BACK ? umma_smem_desc_mn_sw128(sa + k16 * 16 * 128, BOX_BYTES, 1024) : umma_smem_desc_k_sw128(sa + k16 * 32);
-                    const uint64_t bdesc = umma_smem_desc_k_sw128(sb + k16 * 32);
-                    umma_bf16(d_tmem, adesc, bdesc, idesc, (kb != 0 || k16 != 0) ? 1u : 0u);
+            if (u.halves == 0) continue;
+            const uint32_t d0 = tmem_base + static_cast<uint32_t>(buf * TILE_N), d1 = tmem_base + static_cast<uint32_t>((buf ^ 1) * TILE_N);
+            if (!acquire(buf, it)) { ok = false; break; }
+            // While the epilogue still reads the second accumulator, the first half of the k-steps that fit the ring.
+            int lead = 0;
+            if (u.halves == 2) {
+                lead = kblocks < LP_STAGES ? kblocks : LP_STAGES;
+                int sl = s;
+                uint32_t phl = ph;
+                for (int kb = 0; kb < lead; ++kb) {
+                    if (!bounded_wait_hot(smem_u32(&bar_full[sl]), phl, wc, 3u, it)) { ok = false; break; }
+                    tc_fence_after_sync();
+                    multiply(sl, 0, d0, kb == 0);
+                    if (++sl == LP_STAGES) { sl = 0; phl ^= 1u; }
                 }
+                if (!ok || !acquire(buf ^ 1, it)) { ok = false; break; }
+            }
+            for (int kb = 0; kb < kblocks; ++kb) {
+                if (kb >= lead) {
+                    if (!bounded_wait_hot(smem_u32(&bar_full[s]), ph, wc, 3u, it)) { ok = false; break; }
+                    tc_fence_after_sync();
+                    multiply(s, 0, d0, kb == 0);
+                }
+                if (kb == kblocks - 1) umma_commit_pair(smem_u32(&bar_acc_full[buf]));
+                if (u.halves == 2) multiply(s, 1, d1, kb == 0);
                 umma_commit_pair(smem_u32(&bar_empty[s]));
                 if (++s == LP_STAGES) { s = 0; ph ^= 1u; }
             }
             if (!ok) break;
-            umma_commit_pair(smem_u32(&bar_acc_full[buf]));
-            acc_ph ^= 1u << buf;
-            buf ^= 1;
+            if (u.halves == 2) umma_commit_pair(smem_u32(&bar_acc_full[buf ^ 1]));
+            else buf ^= 1;
         }
         if (!ok) {
             // Make sure no MMA is still writing TMEM when it is released.
@@ -484,7 +542,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_consta
         const int grp = (warp - 4) >> 2;                            // takes k-steps grp, grp + LP_LOOK_GROUPS, ... of the launch
         const int r = ((warp - 4) & 3) * 32 + lane;                 // forward: channel; backward: channel r % 64, columns 64 (r / 64) ..
         const uint32_t slot = BACK ? static_cast<uint32_t>((r >> 6) * BOX_BYTES + (r & 63) * 128) : static_cast<uint32_t>(r * 128);
-        const uint32_t code_at = 2 * LP_SLOT_BYTES + (BACK ? static_cast<uint32_t>((r & 63) * 64 + (r >> 6) * 32) : static_cast<uint32_t>(r * 32));
+        const uint32_t code_at = BACK ? static_cast<uint32_t>((r & 63) * 64 + (r >> 6) * 32) : static_cast<uint32_t>(r * 32);
         const uint32_t xor7 = static_cast<uint32_t>(r & 7);
         // Backward: the levels of channel r % 64 of k-step kb, asked for a k-step of the group ahead.
         struct Levels {
@@ -496,21 +554,29 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_consta
             t.b = ld_u32x4(tb + 1);
         };
         LevelPlanes lv;
-        int s = grp;
-        uint32_t ph = 0;
+        int s = grp, c = grp;
+        uint32_t ph = 0, cph = 0;
         int kb = grp, it = 0, levels_of = -1;
         bool ok = true;
         LinearUnit u;
         bool valid = linear_unit(p, pair, 0, u);
         auto settle = [&]() {                                       // into the tile that the k-step lies in
-            while (valid && kb >= kblocks) {
-                kb -= kblocks;
+            while (valid && (u.halves == 0 || kb >= kblocks)) {
+                if (u.halves != 0) kb -= kblocks;
                 valid = linear_unit(p, pair, ++it, u);
             }
         };
         settle();
         Levels ahead{};
         if (BACK && valid) levels_at(kb * TILE_K + (r & 63), ahead);
+        // Every lane waits through lane 0, then observes the completed phase itself.
+        auto wait = [&](uint32_t bar, uint32_t parity, uint32_t site) {
+            bool got = true;
+            if (lane == 0) got = bounded_wait(bar, parity, wc, site, it);
+            got = __any_sync(0xffffffffu, got && lane == 0);
+            if (got) (void)mbar_try_wait(bar, parity);
+            return got;
+        };
         while (valid) {
             if (BACK) {
                 lv.set(ahead.a, ahead.b);
@@ -522,31 +588,29 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_consta
                 levels_at(u.row0 + static_cast<int>(rank) * CTA_ROWS + r, ahead);
                 lv.set(ahead.a, ahead.b);
             }
-            // the codes are there: the stage has been released before
-            bool got = true;
-            if (lane == 0) got = bounded_wait(smem_u32(&bar_codes[s]), ph, wc, 6u, it);
-            got = __any_sync(0xffffffffu, got && lane == 0);
-            if (!got) { ok = false; break; }
-            (void)mbar_try_wait(smem_u32(&bar_codes[s]), ph);                // every lane observes the completed phase
-            const uint32_t stage = ring + s * LP_STAGE_BYTES, base = stage + slot;
+            if (!wait(smem_u32(&bar_codes[c]), cph, 6u)) { ok = false; break; }
+            const uint4 c0 = ld_shared_16(code_ring + c * LP_CODE_BYTES + code_at), c1 = ld_shared_16(code_ring + c * LP_CODE_BYTES + code_at + 16);
+            if (!wait(smem_u32(&bar_empty[s]), ph ^ 1u, 8u)) { ok = false; break; }
+            const uint32_t base = ring + s * LP_STAGE_BYTES + slot;
             // the last, ragged k-step: no level meets padding (infinite ones would make it NaN)
             const int end = BACK ? p.d_out - (kb * TILE_K + (r & 63)) > 0 ? TILE_K : 0 : p.d_in - kb * TILE_K;
+            const uint32_t w[8] = {c0.x, c0.y, c0.z, c0.w, c1.x, c1.y, c1.z, c1.w};
 #pragma unroll
-            for (int q = 0; q < 2; ++q) {
-                const uint4 c = ld_shared_16(stage + code_at + 16 * q);
-                const uint32_t w[4] = {c.x, c.y, c.z, c.w};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    uint4 v = lv.look<WIDE>(w[e]);
-                    if (32 * q + 8 * e >= end) v = make_uint4(0u, 0u, 0u, 0u);
-                    st_shared_16(base + ((static_cast<uint32_t>(4 * q + e) ^ xor7) << 4), v);
-                }
+            for (int e = 0; e < 8; ++e) {
+                uint4 v = lv.look<WIDE>(w[e]);
+                if (8 * e >= end) v = make_uint4(0u, 0u, 0u, 0u);
+                st_shared_16(base + ((static_cast<uint32_t>(e) ^ xor7) << 4), v);
             }
             fence_proxy_async_smem();                // make the stores visible to the tensor core's reads
             __syncwarp();
-            if (lane == 0) mbar_arrive_cluster(map_to_cta(smem_u32(&bar_full[s]), 0));
+            if (lane == 0) {
+                mbar_arrive_cluster(map_to_cta(smem_u32(&bar_full[s]), 0));
+                mbar_arrive(smem_u32(&bar_codes_used[c]));
+            }
             s += LP_LOOK_GROUPS;
             if (s >= LP_STAGES) { s -= LP_STAGES; ph ^= 1u; }
+            c += LP_LOOK_GROUPS;
+            if (c >= LP_CODE_SLOTS) { c -= LP_CODE_SLOTS; cph ^= 1u; }
             kb += LP_LOOK_GROUPS;
             settle();
         }
@@ -555,7 +619,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_consta
         // ------------------------------------------------------------------ epilogue: bias, activation, residual, rounding
         const int ew = warp - (4 + LP_LOOK_WARPS);      // 0..7; four consecutive warps cover the four lane quarters
         const int q = warp & 3;                         // TMEM lane quarter this warp may access
-        const int half = ew >> 2;                       // which 128 of the 256 tokens
+        const int part = ew >> 2;                       // which 128 of a half's 256 tokens
         const bool bf16 = p.bf16 != 0;
         // Lanes 2 i and 2 i + 1 exchange every other token, so that each holds two neighbouring rows of a token: 4-byte accesses.
         const int odd = lane & 1;
@@ -568,72 +632,74 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_consta
             const bool in = row < rows;
             float bias = 0.0f;
             if (!BACK && p.bias && in) bias = half_value(ld_u16(p.bias + row), bf16);
-            if (lane == 0) ok = bounded_wait(smem_u32(&bar_acc_full[buf]), (full_ph >> buf) & 1u, wc, 4u, it);
-            ok = __shfl_sync(0xffffffffu, ok, 0);
-            if (!ok) break;
-            (void)mbar_try_wait(smem_u32(&bar_acc_full[buf]), (full_ph >> buf) & 1u);     // every lane observes the completed phase
-            full_ph ^= 1u << buf;
-            tc_fence_after_sync();
-            const uint32_t tmem_tile = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + static_cast<uint32_t>(buf * TILE_N + half * 128);
-            // even lane: tokens 0, 2, ... of rows (row, row + 1); odd lane: tokens 1, 3, ... of rows (row - 1, row)
-            const long long tok0 = u.tok0 + half * 128 + odd;
+            for (int h = 0; h < u.halves; ++h) {
+                if (lane == 0) ok = bounded_wait(smem_u32(&bar_acc_full[buf]), (full_ph >> buf) & 1u, wc, 4u, it);
+                ok = __shfl_sync(0xffffffffu, ok, 0);
+                if (!ok) break;
+                (void)mbar_try_wait(smem_u32(&bar_acc_full[buf]), (full_ph >> buf) & 1u);     // every lane observes the completed phase
+                full_ph ^= 1u << buf;
+                tc_fence_after_sync();
+                const uint32_t tmem_tile = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + static_cast<uint32_t>(buf * TILE_N + part * 128);
+                // even lane: tokens 0, 2, ... of rows (row, row + 1); odd lane: tokens 1, 3, ... of rows (row - 1, row)
+                const long long tok0 = u.tok0 + h * TILE_N + part * 128 + odd;
 #pragma unroll 1
-            for (int n0 = 0; n0 < 128; n0 += 32) {
-                uint32_t acc[32];
-                tmem_ld_32x32(tmem_tile + static_cast<uint32_t>(n0), acc);
-                tmem_ld_wait();
-                if (n0 == 96) {
-                    tc_fence_before_sync();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive_cluster(map_to_cta(smem_u32(&bar_acc_empty[buf]), 0));
-                }
-                const int left = in ? p.n - static_cast<int>(tok0) - n0 : 0;       // this lane's tokens 0, 2, ... below it exist
-                float2 v[16];
+                for (int n0 = 0; n0 < 128; n0 += 32) {
+                    uint32_t acc[32];
+                    tmem_ld_32x32(tmem_tile + static_cast<uint32_t>(n0), acc);
+                    tmem_ld_wait();
+                    if (n0 == 96) {
+                        tc_fence_before_sync();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive_cluster(map_to_cta(smem_u32(&bar_acc_empty[buf]), 0));
+                    }
+                    const int left = in ? p.n - static_cast<int>(tok0) - n0 : 0;       // this lane's tokens 0, 2, ... below it exist
+                    float2 v[16];
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const float a = __uint_as_float(acc[2 * e]) + bias, b = __uint_as_float(acc[2 * e + 1]) + bias;
-                    const float other = __shfl_xor_sync(0xffffffffu, odd ? a : b, 1);
-                    v[e] = odd ? make_float2(other, b) : make_float2(a, other);
-                }
-                if (!BACK) {
-                    if (p.Z) {
-                        uint16_t *z = p.Z + (tok0 + n0) * p.ld_z + (row - odd);
+                    for (int e = 0; e < 16; ++e) {
+                        const float a = __uint_as_float(acc[2 * e]) + bias, b = __uint_as_float(acc[2 * e + 1]) + bias;
+                        const float other = __shfl_xor_sync(0xffffffffu, odd ? a : b, 1);
+                        v[e] = odd ? make_float2(other, b) : make_float2(a, other);
+                    }
+                    if (!BACK) {
+                        if (p.Z) {
+                            uint16_t *z = p.Z + (tok0 + n0) * p.ld_z + (row - odd);
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            if (2 * e < left) *reinterpret_cast<uint32_t *>(z) = half2_bits(v[e].x, v[e].y, bf16);
-                            z += 2 * p.ld_z;
+                            for (int e = 0; e < 16; ++e) {
+                                if (2 * e < left) *reinterpret_cast<uint32_t *>(z) = half2_bits(v[e].x, v[e].y, bf16);
+                                z += 2 * p.ld_z;
+                            }
+                        }
+                        uint32_t res[16];
+                        if (p.residual) {
+                            const uint16_t *at = p.residual + (tok0 + n0) * p.ld_r + (row - odd);
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) {
+                                res[e] = 2 * e < left ? *reinterpret_cast<const uint32_t *>(at) : 0u;
+                                at += 2 * p.ld_r;
+                            }
+                        }
+                        if (p.act != LIN_NONE) {
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) v[e] = make_float2(activate(v[e].x, p.act), activate(v[e].y, p.act));
+                        }
+                        if (p.residual) {
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) {
+                                const float2 t = half2_value(res[e], bf16);
+                                v[e].x += t.x;
+                                v[e].y += t.y;
+                            }
                         }
                     }
-                    uint32_t res[16];
-                    if (p.residual) {
-                        const uint16_t *at = p.residual + (tok0 + n0) * p.ld_r + (row - odd);
+                    uint16_t *out = p.out + (tok0 + n0) * p.ld_out + (row - odd);
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            res[e] = 2 * e < left ? *reinterpret_cast<const uint32_t *>(at) : 0u;
-                            at += 2 * p.ld_r;
-                        }
-                    }
-                    if (p.act != LIN_NONE) {
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) v[e] = make_float2(activate(v[e].x, p.act), activate(v[e].y, p.act));
-                    }
-                    if (p.residual) {
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            const float2 t = half2_value(res[e], bf16);
-                            v[e].x += t.x;
-                            v[e].y += t.y;
-                        }
+                    for (int e = 0; e < 16; ++e) {
+                        if (2 * e < left) *reinterpret_cast<uint32_t *>(out) = half2_bits(v[e].x, v[e].y, bf16);
+                        out += 2 * p.ld_out;
                     }
                 }
-                uint16_t *out = p.out + (tok0 + n0) * p.ld_out + (row - odd);
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    if (2 * e < left) *reinterpret_cast<uint32_t *>(out) = half2_bits(v[e].x, v[e].y, bf16);
-                    out += 2 * p.ld_out;
-                }
+                buf ^= 1;
             }
-            buf ^= 1;
         }
     }
 
