@@ -196,6 +196,8 @@ int32_t device_info(DeviceInfo **out)
         GQ_CUDA(cudaFuncSetAttribute(gq::linear_pair_kernel<false, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, gq::LP_SMEM_BYTES));
         GQ_CUDA(cudaFuncSetAttribute(gq::linear_pair_kernel<true, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, gq::LP_SMEM_BYTES));
         GQ_CUDA(cudaFuncSetAttribute(gq::linear_pair_kernel<true, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, gq::LP_SMEM_BYTES));
+        GQ_CUDA(cudaFuncSetAttribute(gq::linear_token_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, gq::LT_SMEM_BYTES));
+        GQ_CUDA(cudaFuncSetAttribute(gq::linear_token_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, gq::LT_SMEM_BYTES));
         GQ_CUDA(cudaFuncSetAttribute(gq::linear_level_grad_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, gq::LG_SMEM_BYTES));
         GQ_CUDA(cudaFuncSetAttribute(gq::hessian_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                      gq::HS_SMEM_BYTES));
@@ -1561,9 +1563,8 @@ int32_t gq_linear(const void *X, int32_t dtype, int64_t n, int64_t d_in, int64_t
     while (ranks < gq::LT_MAX_CLUSTER && groups * ranks < static_cast<unsigned>(di->sm_count) && pieces >= 2 * ranks * gq::LT_WARPS) ranks *= 2;
     {
         LaunchScope scope(GQ_KERNEL_LINEAR, st);
-        const auto kernel = p.bf16 ? (m > 8 ? gq::linear_token_kernel<true, true> : gq::linear_token_kernel<true, false>)
-                                   : (m > 8 ? gq::linear_token_kernel<false, true> : gq::linear_token_kernel<false, false>);
-        launch_cluster(kernel, ranks, dim3(groups * ranks), gq::LT_THREADS, 0, st, p, static_cast<int>(ranks));
+        launch_cluster(p.bf16 ? gq::linear_token_kernel<true> : gq::linear_token_kernel<false>, ranks, dim3(groups * ranks), gq::LT_THREADS,
+                       gq::LT_SMEM_BYTES, st, p, static_cast<int>(ranks));
     }
     GQ_CUDA(cudaGetLastError());
     return GQ_OK;

@@ -6,13 +6,11 @@
 // Layout (linear_pack_kernel): codes [d_out][ld] bytes, two codes a byte, the lower four bits first, ld = 16 ceil(d_in / 32);
 // table [d_out][16] in the activations' type (bf16 or fp16), zero from m on.
 //
-// A level is looked up in registers: a channel's 16 levels are kept as two planes of 16 bytes (low and high bytes, eight
+// On the tensor cores' path a level is looked up in registers: a channel's 16 levels are kept as two planes of 16 bytes (low and high bytes, eight
 // registers), and a byte permutation looks four codes up in eight bytes at once.  For four weights: two permutations a plane (levels
 // 0..7 and 8..15), one that takes either by the codes' top bits, and two that join the planes: 2.6 integer instructions a weight, 1.3
-// where m <= 8.  Shared-memory tables would need a load per weight or per pair, with conflicts between the lanes' random codes.
-//
-// Few tokens (linear_token_kernel, n <= 8): bound by the codes' bytes and, behind them, the lookups.  More tokens
-// (linear_pair_kernel): tensor cores, the weight operand written to shared memory by eight lookup warps.
+// where m <= 8.  Few tokens (linear_token_kernel, n <= 8) are bound by the codes' bytes and, behind them, the lookups, and use tables in
+// shared memory.  More tokens (linear_pair_kernel): tensor cores, the weight operand written to shared memory by eight lookup warps.
 #pragma once
 #include <cuda.h>
 #include <cuda_bf16.h>
@@ -178,12 +176,15 @@ struct LinearParams {
 };
 
 constexpr int LT_WARPS = 8;
-constexpr int LT_THREADS = 32 * LT_WARPS;
+constexpr int LT_THREADS = 32 * LT_WARPS;         // a thread per pair of codes when the tables are built
 constexpr int LT_CHANNELS = 16;
 constexpr int LT_TOKENS = 8;
 constexpr int LT_K = 128;                 // contraction indices a warp takes at a time: 32 per lane of a quad
 constexpr int LT_MAX_CLUSTER = 8;
-constexpr int LT_AHEAD = 4;               // even
+constexpr int LT_AHEAD = 4;               // a multiple of LT_X_AHEAD
+constexpr int LT_X_AHEAD = 2;
+constexpr int LT_TABLE_BYTES = 256 * 128;         // levels of all pairs of codes for 8 channels, a word per lane
+constexpr int LT_SMEM_BYTES = 2 * LT_TABLE_BYTES + 32768;      // the tables start at a multiple of their size
 
 template <bool BF16>
 __device__ __forceinline__ void mma_m16n8k16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
@@ -202,76 +203,124 @@ __device__ __forceinline__ void mma_m16n8k16(float (&c)[4], uint32_t a0, uint32_
 // inside a piece is free as long as both operands share it: lane (g, t) of a quad takes the 32 codes 32 t .. 32 t + 31 of
 // channels g and g + 8 (16 bytes each) and token g's activations at the same place, four codes a product and lane, so that codes
 // are read 64 contiguous bytes a channel and nothing is exchanged between lanes.
-template <bool BF16, bool WIDE>
-__global__ void __launch_bounds__(LT_THREADS) linear_token_kernel(const LinearParams p, int ranks)
+//
+// Lookups: a byte of codes names two levels, which stand side by side in a table of 256 words for the channel.  Every lane has its
+// own copy in its own bank (row = byte, word = lane: 32 KB for 8 channels), so 32 random bytes meet no conflicts: a load and two integer
+// instructions for two weights, where looking them up in registers takes more than five.
+template <bool BF16>
+__global__ void __launch_bounds__(LT_THREADS, 2) linear_token_kernel(const LinearParams p, int ranks)
 {
+    extern __shared__ uint8_t smem_raw[];
     __shared__ float sums[LT_WARPS][LT_TOKENS][LT_CHANNELS];
     __shared__ float mine[LT_TOKENS * LT_CHANNELS];
+    __shared__ uint16_t levels[LT_CHANNELS][LIN_LEVELS];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
     const int group = static_cast<int>(blockIdx.x) / ranks, rank = static_cast<int>(blockIdx.x) - group * ranks;
     const int j0 = group * LT_CHANNELS;
+    const uint32_t tables = (smem_u32(smem_raw) + 32767u) & ~32767u;
     griddep_launch();
     griddep_wait();
     // channels are a multiple of 8, so either all of g or all of g + 8 are there
     const bool second = j0 + 8 < p.d_out;
     const int ja = j0 + g, jb = second ? ja + 8 : ja;
-    LevelPlanes la, lb;
-    {
-        const uint4 *ta = reinterpret_cast<const uint4 *>(p.table + static_cast<size_t>(ja) * LIN_LEVELS);
-        const uint4 *tb = reinterpret_cast<const uint4 *>(p.table + static_cast<size_t>(jb) * LIN_LEVELS);
-        const uint4 a0 = ld_u32x4(ta), a1 = ld_u32x4(ta + 1), b0 = ld_u32x4(tb), b1 = ld_u32x4(tb + 1);
-        la.set(a0, a1);
-        lb.set(b0, b1);
-    }
     const uint8_t *ca = p.codes + static_cast<size_t>(ja) * p.ld_codes, *cb = p.codes + static_cast<size_t>(jb) * p.ld_codes;
     const uint16_t *x = p.X + static_cast<long long>(g < p.n ? g : 0) * p.ld_x;
     const bool have = g < p.n;
-    float c0[4] = {0.f, 0.f, 0.f, 0.f}, c1[4] = {0.f, 0.f, 0.f, 0.f};
     const int pieces = (p.d_in + LT_K - 1) / LT_K, stride = ranks * LT_WARPS;
-    struct Codes {
-        uint4 a, b;
-    };
-    struct Tokens {
-        uint4 x[4];
-    };
-    auto fetch_codes = [&](int piece, Codes &f) {
-        const int k = piece * LT_K + 32 * t;
-        const bool in = piece < pieces && k < p.d_in;
-        f.a = in ? ld_once_16(reinterpret_cast<const uint4 *>(ca + (k >> 1))) : make_uint4(0u, 0u, 0u, 0u);
-        f.b = in ? ld_once_16(reinterpret_cast<const uint4 *>(cb + (k >> 1))) : make_uint4(0u, 0u, 0u, 0u);
-    };
-    auto fetch_tokens = [&](int piece, Tokens &f) {
-        const int k = piece * LT_K + 32 * t;
+    // A warp's pieces are rank * LT_WARPS + warp, + stride, ...; the `whole` first of them lie inside the row, one ragged piece may follow.
+    // Codes are asked for LT_AHEAD pieces ahead (they come from device memory), activations LT_X_AHEAD (from L2 or L1).
+    const int first = rank * LT_WARPS + warp, full = p.d_in / LT_K;
+    const int whole = first < full ? (full - first + stride - 1) / stride : 0;
+    const bool ragged = full < pieces && full % stride == first;
+    const uint8_t *qa = ca + (first * LT_K + 32 * t) / 2, *qb = cb + (first * LT_K + 32 * t) / 2;
+    const uint16_t *xt = x + first * LT_K + 32 * t;
+    const size_t code_step = static_cast<size_t>(stride) * LT_K / 2, x_step = static_cast<size_t>(stride) * LT_K;
+    uint4 codes[LT_AHEAD][2], tokens[LT_X_AHEAD][4];
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-            f.x[q] = (piece < pieces && have && k + 8 * q < p.d_in) ? ld_u32x4(x + k + 8 * q) : make_uint4(0u, 0u, 0u, 0u);
+    for (int d = 0; d < LT_X_AHEAD; ++d)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) tokens[d][q] = make_uint4(0u, 0u, 0u, 0u);      // stays so in lanes without a token
+    auto fetch_codes = [&](int i, uint4 (&f)[2]) {
+        if (i < whole) {
+            f[0] = ld_once_16(reinterpret_cast<const uint4 *>(qa));
+            f[1] = ld_once_16(reinterpret_cast<const uint4 *>(qb));
+        }
+        qa += code_step;
+        qb += code_step;
     };
-    auto use = [&](int piece, const Codes &f, const Tokens &y) {
-        const uint32_t qa[4] = {f.a.x, f.a.y, f.a.z, f.a.w}, qb[4] = {f.b.x, f.b.y, f.b.z, f.b.w};
-        const bool ragged = (piece + 1) * LT_K > p.d_in;
+    auto fetch_tokens = [&](int i, uint4 (&f)[4]) {
+        if (i < whole && have) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) f[q] = ld_u32x4(xt + 8 * q);
+        }
+        xt += x_step;
+    };
+#pragma unroll
+    for (int d = 0; d < LT_AHEAD; ++d) fetch_codes(d, codes[d]);
+    // the levels of 16 channels: 512 bytes
+    if (tid < LT_CHANNELS * LIN_LEVELS / 2) {
+        const int ch = tid / (LIN_LEVELS / 2), j = j0 + ch < p.d_out ? j0 + ch : j0;
+        reinterpret_cast<uint32_t *>(&levels[ch][0])[tid % (LIN_LEVELS / 2)] =
+            *(reinterpret_cast<const uint32_t *>(p.table + static_cast<size_t>(j) * LIN_LEVELS) + tid % (LIN_LEVELS / 2));
+    }
+#pragma unroll
+    for (int d = 0; d < LT_X_AHEAD; ++d) fetch_tokens(d, tokens[d]);
+    __syncthreads();
+    // Thread = pair of codes; eight threads next to each other store to eight different channels' words of their rows.
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int ch = (i + tid) & 7;
+            const uint32_t v = static_cast<uint32_t>(levels[8 * h + ch][tid & 15]) | (static_cast<uint32_t>(levels[8 * h + ch][tid >> 4]) << 16);
+            st_shared_16(tables + h * LT_TABLE_BYTES + tid * 128 + ch * 16, make_uint4(v, v, v, v));
+        }
+    __syncthreads();
+    float c0[4] = {0.f, 0.f, 0.f, 0.f}, c1[4] = {0.f, 0.f, 0.f, 0.f};
+    const uint32_t mine_a = tables + lane * 4, mine_b = mine_a + LT_TABLE_BYTES;
+    auto word = [](uint32_t base, uint32_t w, int byte) {
+        const uint32_t row = (byte == 0 ? w << 7 : w >> (8 * byte - 7)) & 0x7F80u;
+        uint32_t v;
+        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(row | base));
+        return v;
+    };
+    auto use = [&](const uint4 (&f)[2], const uint4 (&y)[4], int end) {
+        const uint32_t qa[4] = {f[0].x, f[0].y, f[0].z, f[0].w}, qb[4] = {f[1].x, f[1].y, f[1].z, f[1].w};
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            uint4 wa = la.look<WIDE>(qa[q]), wb = lb.look<WIDE>(qb[q]);
-            if (ragged && piece * LT_K + 32 * t + 8 * q >= p.d_in) wa = wb = make_uint4(0u, 0u, 0u, 0u);      // no level meets padding
-            mma_m16n8k16<BF16>(c0, wa.x, wb.x, wa.y, wb.y, y.x[q].x, y.x[q].y);
-            mma_m16n8k16<BF16>(c1, wa.z, wb.z, wa.w, wb.w, y.x[q].z, y.x[q].w);
+            uint32_t wa[4], wb[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                wa[e] = word(mine_a, qa[q], e);
+                wb[e] = word(mine_b, qb[q], e);
+            }
+            if (8 * q >= end) {                                       // (never in a whole piece) no level meets padding
+#pragma unroll
+                for (int e = 0; e < 4; ++e) wa[e] = wb[e] = 0u;
+            }
+            mma_m16n8k16<BF16>(c0, wa[0], wb[0], wa[1], wb[1], y[q].x, y[q].y);
+            mma_m16n8k16<BF16>(c1, wa[2], wb[2], wa[3], wb[3], y[q].z, y[q].w);
         }
     };
-    // Codes are asked for LT_AHEAD pieces ahead (they come from device memory), activations one piece ahead (from L2 or L1).
-    int piece = rank * LT_WARPS + warp;
-    Codes codes[LT_AHEAD];
-    Tokens tokens[2];
-#pragma unroll
-    for (int d = 0; d < LT_AHEAD; ++d) fetch_codes(piece + d * stride, codes[d]);
-    fetch_tokens(piece, tokens[0]);
-    while (piece < pieces) {
+    for (int i = 0; i < whole; i += LT_AHEAD) {
 #pragma unroll
         for (int d = 0; d < LT_AHEAD; ++d) {
-            fetch_tokens(piece + stride, tokens[(d + 1) & 1]);
-            use(piece, codes[d], tokens[d & 1]);                  // nothing but zeros past the end
-            fetch_codes(piece + LT_AHEAD * stride, codes[d]);
-            piece += stride;
+            if (i + d >= whole) break;
+            use(codes[d], tokens[d % LT_X_AHEAD], LT_K);
+            fetch_codes(i + d + LT_AHEAD, codes[d]);
+            fetch_tokens(i + d + LT_X_AHEAD, tokens[d % LT_X_AHEAD]);
         }
+    }
+    if (ragged) {
+        const int k = full * LT_K + 32 * t;
+        uint4 f[2] = {make_uint4(0u, 0u, 0u, 0u), make_uint4(0u, 0u, 0u, 0u)}, y[4];
+        if (k < p.d_in) {
+            f[0] = ld_once_16(reinterpret_cast<const uint4 *>(ca + (k >> 1)));
+            f[1] = ld_once_16(reinterpret_cast<const uint4 *>(cb + (k >> 1)));
+        }
+#pragma unroll
+        for (int q = 0; q < 4; ++q) y[q] = (have && k + 8 * q < p.d_in) ? ld_u32x4(x + k + 8 * q) : make_uint4(0u, 0u, 0u, 0u);
+        use(f, y, p.d_in - k);
     }
     // c[0], c[1]: channel g, tokens 2 t, 2 t + 1; c[2], c[3]: channel g + 8
 #pragma unroll
