@@ -115,6 +115,7 @@ struct DeviceInfo {
     bool ready = false;
     int sm_count = 0;
     int max_pairs = 0;          // CTA pairs (clusters of two) of a tensor-core kernel that can be resident at once
+    int split_clusters[2] = {0, 0};      // clusters of two and of four pairs of linear_pair_kernel that can be
     uint32_t *status_ptr = nullptr;
 };
 DeviceInfo g_dev[kMaxDevices];
@@ -192,10 +193,14 @@ int32_t device_info(DeviceInfo **out)
         GQ_CUDA(cudaFuncSetAttribute(gq::cd_block_kernel<8, 16>, cudaFuncAttributeMaxDynamicSharedMemorySize, gq::cd_smem_bytes(16)));
         GQ_CUDA(cudaFuncSetAttribute(gq::cd_block_kernel<16, 32>, cudaFuncAttributeMaxDynamicSharedMemorySize, gq::cd_smem_bytes(32)));
         GQ_CUDA(cudaFuncSetAttribute(gq::cd_block_kernel<16, 16>, cudaFuncAttributeMaxDynamicSharedMemorySize, gq::cd_smem_bytes(16)));
-        GQ_CUDA(cudaFuncSetAttribute(gq::linear_pair_kernel<false, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, gq::LP_SMEM_BYTES));
-        GQ_CUDA(cudaFuncSetAttribute(gq::linear_pair_kernel<false, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, gq::LP_SMEM_BYTES));
-        GQ_CUDA(cudaFuncSetAttribute(gq::linear_pair_kernel<true, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, gq::LP_SMEM_BYTES));
-        GQ_CUDA(cudaFuncSetAttribute(gq::linear_pair_kernel<true, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, gq::LP_SMEM_BYTES));
+        GQ_CUDA(cudaFuncSetAttribute(gq::linear_pair_kernel<false, false, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, gq::LP_SMEM_BYTES));
+        GQ_CUDA(cudaFuncSetAttribute(gq::linear_pair_kernel<false, false, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, gq::LP_SMEM_BYTES));
+        GQ_CUDA(cudaFuncSetAttribute(gq::linear_pair_kernel<false, true, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, gq::LP_SMEM_BYTES));
+        GQ_CUDA(cudaFuncSetAttribute(gq::linear_pair_kernel<false, true, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, gq::LP_SMEM_BYTES));
+        GQ_CUDA(cudaFuncSetAttribute(gq::linear_pair_kernel<true, false, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, gq::LP_SMEM_BYTES));
+        GQ_CUDA(cudaFuncSetAttribute(gq::linear_pair_kernel<true, false, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, gq::LP_SMEM_BYTES));
+        GQ_CUDA(cudaFuncSetAttribute(gq::linear_pair_kernel<true, true, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, gq::LP_SMEM_BYTES));
+        GQ_CUDA(cudaFuncSetAttribute(gq::linear_pair_kernel<true, true, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, gq::LP_SMEM_BYTES));
         GQ_CUDA(cudaFuncSetAttribute(gq::linear_token_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, gq::LT_SMEM_BYTES));
         GQ_CUDA(cudaFuncSetAttribute(gq::linear_token_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, gq::LT_SMEM_BYTES));
         GQ_CUDA(cudaFuncSetAttribute(gq::linear_level_grad_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, gq::LG_SMEM_BYTES));
@@ -222,6 +227,25 @@ int32_t device_info(DeviceInfo **out)
             if (clusters > di.sm_count / 2) clusters = di.sm_count / 2;
             if (clusters < 1) clusters = 1;
             di.max_pairs = clusters;
+        }
+        for (int i = 0; i < 2; ++i) {
+            cudaLaunchConfig_t cfg = {};
+            cudaLaunchAttribute attr;
+            attr.id = cudaLaunchAttributeClusterDimension;
+            attr.val.clusterDim.x = static_cast<unsigned>(4 << i);
+            attr.val.clusterDim.y = 1;
+            attr.val.clusterDim.z = 1;
+            cfg.gridDim = dim3(static_cast<unsigned>(di.sm_count / (4 << i) * (4 << i)));
+            cfg.blockDim = dim3(gq::LP_THREADS);
+            cfg.dynamicSmemBytes = gq::LP_SMEM_BYTES;
+            cfg.attrs = &attr;
+            cfg.numAttrs = 1;
+            int clusters = 0;
+            if (cudaOccupancyMaxActiveClusters(&clusters, gq::linear_pair_kernel<false, true, true>, &cfg) != cudaSuccess) {
+                (void)cudaGetLastError();
+                clusters = 0;
+            }
+            di.split_clusters[i] = clusters;
         }
         if (!g_encode) {
             void *fn = nullptr;
@@ -252,14 +276,14 @@ unsigned long long wait_budget_ns()
 }
 
 // 16-bit tensor [groups][rows][features] (bf16 unless `dtype` says fp16; row stride ld, group stride gstride, in elements) as a TMA map
-// with 64-feature x 64-row boxes and the 128-byte swizzle.
+// with boxes of 64 features x `box_rows` rows (64 unless given) and the 128-byte swizzle.
 int32_t make_map(CUtensorMap *map, const void *base, int64_t features, int64_t rows, int64_t groups, int64_t ld,
-                 int64_t gstride, CUtensorMapDataType dtype = CU_TENSOR_MAP_DATA_TYPE_BFLOAT16)
+                 int64_t gstride, CUtensorMapDataType dtype = CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, int box_rows = gq::TILE_K)
 {
     cuuint64_t dims[3] = {static_cast<cuuint64_t>(features), static_cast<cuuint64_t>(rows),
                           static_cast<cuuint64_t>(groups)};
     cuuint64_t strides[2] = {static_cast<cuuint64_t>(ld) * 2, static_cast<cuuint64_t>(gstride) * 2};
-    cuuint32_t box[3] = {gq::BOX_FEATURES, gq::TILE_K, 1};
+    cuuint32_t box[3] = {gq::BOX_FEATURES, static_cast<cuuint32_t>(box_rows), 1};
     cuuint32_t estr[3] = {1, 1, 1};
     CUresult r = g_encode(map, dtype, 3, const_cast<void *>(base), dims, strides, box, estr,
                           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
@@ -290,14 +314,14 @@ int32_t make_map_f32(CUtensorMap *map, const float *base, int64_t cols, int64_t 
 }
 
 // Bytes [rows][width] (width a multiple of 16) as a TMA map with boxes of `box_width` bytes x `box_rows` rows.
-int32_t make_map_bytes(CUtensorMap *map, const void *base, int64_t width, int64_t rows, int box_width, int box_rows)
+int32_t make_map_bytes(CUtensorMap *map, const void *base, int64_t width, int64_t rows, int box_width, int box_rows, CUtensorMapSwizzle swizzle)
 {
     cuuint64_t dims[3] = {static_cast<cuuint64_t>(width), static_cast<cuuint64_t>(rows), 1};
     cuuint64_t strides[2] = {static_cast<cuuint64_t>(width), static_cast<cuuint64_t>(width) * static_cast<cuuint64_t>(rows)};
     cuuint32_t box[3] = {static_cast<cuuint32_t>(box_width), static_cast<cuuint32_t>(box_rows), 1};
     cuuint32_t estr[3] = {1, 1, 1};
     CUresult r = g_encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void *>(base), dims, strides, box, estr,
-                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                          CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) {
         tl_last_cuda_error = static_cast<int32_t>(cudaErrorInvalidValue);
@@ -1496,17 +1520,35 @@ static int32_t linear_pair(bool back, gq::LinearParams p, int32_t dtype, const v
     p.doubles = static_cast<int>(2 * rest <= di->max_pairs && p.n > gq::TILE_N ? tiles - rest : tiles);
     p.units = p.doubles + 2 * (static_cast<int>(tiles) - p.doubles);
     p.pairs = p.units < di->max_pairs ? p.units : di->max_pairs;
+    // Few tiles of 256 x 256: the contraction is split over the pairs of a cluster, up to four of them with four k-steps each at least,
+    // while all clusters are resident at once (4096 x 4096, 256 tokens: 16 clusters of eight CTAs, two of which wait for the others,
+    // take 45 us, of four CTAs 37).
+    const int64_t singles = row_tiles * ((p.n + gq::TILE_N - 1) / gq::TILE_N);
+    const int ksteps = (kdim + gq::TILE_K - 1) / gq::TILE_K;
+    p.ranks = 1;
+    while (p.ranks < gq::LP_MAX_SPLIT && singles <= di->split_clusters[p.ranks - 1] && ksteps >= 8 * p.ranks) p.ranks *= 2;
+    const bool split = p.ranks > 1;
+    if (split) p.pairs = static_cast<int>(singles) * p.ranks;
+    p.ntile = p.n < gq::TILE_N ? (p.n + 31) / 32 * 32 : gq::TILE_N;
     p.status = di->status_ptr;
     p.wait_budget_ns = wait_budget_ns();
+    p.box_rows = split && p.ntile / 2 < gq::TILE_K ? p.ntile / 2 : gq::TILE_K;
     CUtensorMap map, map_codes;
-    if (int32_t rc = make_map(&map, in, kdim, p.n, 1, ld_in, static_cast<int64_t>(p.n) * ld_in, map_type(dtype))) return rc;
-    // a k-step's codes: 128 channels x 32 bytes forward, 64 channels x 64 bytes backward
-    if (int32_t rc = make_map_bytes(&map_codes, p.codes, p.ld_codes, p.d_out, back ? 64 : 32, back ? gq::TILE_K : gq::CTA_ROWS)) return rc;
+    if (int32_t rc = make_map(&map, in, kdim, p.n, 1, ld_in, static_cast<int64_t>(p.n) * ld_in, map_type(dtype), p.box_rows)) return rc;
+    // the codes of four k-steps: 128 channels x 128 bytes forward, 256 channels x 64 bytes backward
+    if (int32_t rc = make_map_bytes(&map_codes, p.codes, p.ld_codes, p.d_out, back ? 64 : 128, back ? 4 * gq::TILE_K : gq::CTA_ROWS,
+                                    back ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B))
+        return rc;
     {
         LaunchScope scope(GQ_KERNEL_LINEAR, st);
-        const auto kernel = back ? (m > 8 ? gq::linear_pair_kernel<true, true> : gq::linear_pair_kernel<true, false>)
-                                 : (m > 8 ? gq::linear_pair_kernel<false, true> : gq::linear_pair_kernel<false, false>);
-        launch(kernel, dim3(static_cast<unsigned>(2 * p.pairs)), gq::LP_THREADS, gq::LP_SMEM_BYTES, st, map, map_codes, p);
+        const bool wide = m > 8;
+        const auto kernel =
+            split ? (back ? (wide ? gq::linear_pair_kernel<true, true, true> : gq::linear_pair_kernel<true, false, true>)
+                          : (wide ? gq::linear_pair_kernel<false, true, true> : gq::linear_pair_kernel<false, false, true>))
+                  : (back ? (wide ? gq::linear_pair_kernel<true, true, false> : gq::linear_pair_kernel<true, false, false>)
+                          : (wide ? gq::linear_pair_kernel<false, true, false> : gq::linear_pair_kernel<false, false, false>));
+        launch_cluster(kernel, static_cast<unsigned>(2 * p.ranks), dim3(static_cast<unsigned>(2 * p.pairs)), gq::LP_THREADS, gq::LP_SMEM_BYTES, st, map,
+                       map_codes, p);
     }
     GQ_CUDA(cudaGetLastError());
     return GQ_OK;

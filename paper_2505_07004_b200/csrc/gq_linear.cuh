@@ -171,6 +171,7 @@ struct LinearParams {
     long long ld_x;
     // pair kernel
     int row_tiles, tok_tiles, doubles, units, pairs;      // tiles of 256 rows, of 512 tokens
+    int ranks, ntile, box_rows;                           // shares of the contraction, columns of a tile, tokens of a TMA box (SPLIT)
     uint32_t *status;
     unsigned long long wait_budget_ns;
 };
@@ -355,13 +356,15 @@ constexpr int LP_SLOT_BYTES = (CTA_ROWS / BOX_FEATURES) * BOX_BYTES;      // one
 constexpr int LP_HALVES = 2;                                              // token tiles of 256 that share a weight operand
 constexpr int LP_STAGES = 4;
 constexpr int LP_STAGE_BYTES = (1 + LP_HALVES) * LP_SLOT_BYTES;           // [weights | tokens | tokens]
-constexpr int LP_CODE_BYTES = CTA_ROWS * TILE_K / 2;                      // codes of an operand block: 4 KB
-constexpr int LP_CODE_SLOTS = 8;
+constexpr int LP_CODE_KSTEPS = 4;                                         // k-steps whose codes come together
+constexpr int LP_CODE_BYTES = LP_CODE_KSTEPS * CTA_ROWS * TILE_K / 2;     // 16 KB
+constexpr int LP_CODE_SLOTS = 2;
 constexpr int LP_LOOK_GROUPS = 2;                                         // of four warps; they take the k-steps in turn
 constexpr int LP_LOOK_WARPS = 4 * LP_LOOK_GROUPS;
 constexpr int LP_EPI_WARPS = 8;
 constexpr int LP_THREADS = 32 * (4 + LP_LOOK_WARPS + LP_EPI_WARPS);
 constexpr int LP_SMEM_BYTES = LP_STAGES * LP_STAGE_BYTES + LP_CODE_SLOTS * LP_CODE_BYTES + 1024;
+constexpr int LP_MAX_SPLIT = 4;                                           // pairs of a cluster (eight CTAs)
 constexpr int LG_STAGES = 6;                                              // gradient of the levels
 constexpr int LG_STAGE_BYTES = 2 * LP_SLOT_BYTES;                         // [dZ | tokens]
 constexpr int LG_SMEM_BYTES = LG_STAGES * LG_STAGE_BYTES + LP_EPI_WARPS * LIN_LEVELS * 32 * 4 + 1024;
@@ -388,14 +391,58 @@ __host__ __device__ constexpr uint32_t umma_idesc_16(uint32_t m, uint32_t n, boo
            ((n >> 3) << 17) | ((m >> 4) << 24);
 }
 
+// umma_commit_pair where the pair's first CTA has rank `leader` in its cluster.
+__device__ __forceinline__ void umma_commit_pair_at(uint32_t leader, uint32_t bar)
+{
+    const uint16_t mask = static_cast<uint16_t>(3u << leader);
+    asm volatile(
+        "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+        ::"r"(bar), "h"(mask)
+        : "memory");
+}
+__device__ __forceinline__ void st_shared_4(uint32_t addr, uint32_t v)
+{
+    asm volatile("st.shared.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
+}
+__device__ __forceinline__ void ld_cluster_f32x4(uint32_t addr, float (&v)[4])
+{
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]) : "r"(addr) : "memory");
+}
+
+// One lane of a converged warp, always the same one.
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok));
+    return ok != 0;
+}
+// bounded_wait_hot for a whole warp, the same answer in all lanes.
+__device__ __forceinline__ bool warp_wait_hot(uint32_t bar, uint32_t parity, const WaitCtx &w, uint32_t site, uint32_t unit)
+{
+    if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+    const uint64_t t0 = global_timer_ns();
+    for (uint32_t spins = 1;; ++spins) {
+        if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+        if ((spins & 63u) == 0u && __any_sync(0xffffffffu, wait_gave_up(w, t0, site, unit))) return false;
+    }
+}
+
 struct LinearUnit {
     int row0, tok0, halves;      // 256 rows of the weights' side, `halves` tiles of 256 tokens from tok0 on
 };
 // The it-th unit of a pair.  Tiles of 256 rows x 512 tokens: the first `doubles` of them whole, the others in two units.  Row tiles in
 // blocks of LP_ROW_BLOCK, inside a block token tiles outermost: tiles worked on at the same time share few token tiles (2 bytes an
 // element) and more row tiles (half a byte).
+template <bool SPLIT>
 __device__ __forceinline__ bool linear_unit(const LinearParams &p, int pair, int it, LinearUnit &u)
 {
+    if (SPLIT) {                 // one tile of at most 256 tokens a cluster
+        const int tok = pair / p.row_tiles;
+        u.row0 = (pair - tok * p.row_tiles) * TILE_M;
+        u.tok0 = tok * TILE_N;
+        u.halves = 1;
+        return it == 0;
+    }
     const int unit = it * p.pairs + pair;
     if (unit >= p.units) return false;
     const int over = unit - p.doubles, tile = over < 0 ? unit : p.doubles + (over >> 1);
@@ -416,17 +463,21 @@ __device__ __forceinline__ bool linear_unit(const LinearParams &p, int pair, int
 // Forward (BACK false): D[channel][token] = sum_c W[channel][c] X[token][c], both operands with the contraction contiguous; a lookup thread
 // owns a channel for the whole tile, its levels stay in registers.  Backward: D[c][token] = sum_j W[j][c] dZ[token][j]; the rows of
 // the weight operand are contraction indices, a lookup thread owns 64 columns of one channel a k-step and reads that channel's levels
-// a step ahead.  Codes come by TMA as well: read by the lookup threads from global memory, 32 bytes of a row each, they cost
-// 28 us of 313 (8192 x 4096 x 4096).  A looked-up operand serves two tiles of 256 tokens, the two accumulators that tensor memory
+// a step ahead.  Codes come by TMA as well, those of four k-steps together: read by the lookup threads from global memory they cost
+// 28 us of 313 (8192 x 4096 x 4096), and boxes of 128 rows of 32 bytes, a k-step each, came once in 850 clocks.  A looked-up operand serves two tiles of 256 tokens, the two accumulators that tensor memory
 // holds: with one tile each, lookups and their stores were in the way of the tensor core (263 us, 221 with the lookups left out).
 // Rows of D are the lanes of tensor memory, so tokens (columns) come in any number without work for the weights' side.
-template <bool BACK, bool WIDE>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LP_THREADS, 1)
+//
+// SPLIT: few tiles.  A cluster of `ranks` pairs works on one tile of 256 rows and up to 256 tokens, a share of the contraction each; the
+// partial sums go to shared memory (where the ring was) and every pair joins a share of the tokens through distributed shared memory.
+// 77 tokens, 1032 -> 3000: 12 pairs instead of one tile each on 12 of 74.
+template <bool BACK, bool WIDE, bool SPLIT>
+__global__ void __launch_bounds__(LP_THREADS, 1)
 linear_pair_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_constant__ CUtensorMap mapC, const LinearParams p)
 {
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t bar_codes[LP_CODE_SLOTS];       // this CTA's codes have come
-    __shared__ __align__(8) uint64_t bar_codes_used[LP_CODE_SLOTS];  // four lookup warps have read them
+    __shared__ __align__(8) uint64_t bar_codes_used[LP_CODE_SLOTS];  // the lookup warps have read them
     __shared__ __align__(8) uint64_t bar_full[LP_STAGES];     // first CTA: bytes of both CTAs + four lookup warps of both
     __shared__ __align__(8) uint64_t bar_empty[LP_STAGES];    // both CTAs: signalled by the MMA commits
     __shared__ __align__(8) uint64_t bar_acc_full[2];         // both CTAs, one per accumulator
@@ -435,18 +486,22 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_consta
     __shared__ uint32_t tmem_base_smem;
     __shared__ volatile uint32_t abort_flag;
 
-    const int warp = threadIdx.x >> 5;
+    const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0);      // (the same for all lanes, and known to be)
     const int lane = threadIdx.x & 31;
-    const uint32_t rank = cluster_ctarank();
-    const int pair = static_cast<int>(blockIdx.x >> 1);
+    const uint32_t rank = cluster_ctarank() & 1u;             // in the pair
+    const uint32_t leader = cluster_ctarank() - rank;         // the pair's first CTA in the cluster
+    const int share = SPLIT ? static_cast<int>(leader >> 1) : 0;
+    const int pair = static_cast<int>(blockIdx.x >> 1) / (SPLIT ? p.ranks : 1);
     const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u, code_ring = ring + LP_STAGES * LP_STAGE_BYTES;
     const int kdim = BACK ? p.d_out : p.d_in, rows = BACK ? p.d_in : p.d_out;
-    const int kblocks = (kdim + TILE_K - 1) / TILE_K;
+    const int ksteps = (kdim + TILE_K - 1) / TILE_K;
+    const int kfirst = SPLIT ? ksteps * share / p.ranks : 0, kblocks = SPLIT ? ksteps * (share + 1) / p.ranks - kfirst : ksteps;
+    const int ntile = SPLIT ? p.ntile : TILE_N;               // columns of an accumulator, half of them from either CTA
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < LP_CODE_SLOTS; ++s) {
             mbar_init(smem_u32(&bar_codes[s]), 1);
-            mbar_init(smem_u32(&bar_codes_used[s]), 4);
+            mbar_init(smem_u32(&bar_codes_used[s]), LP_LOOK_WARPS);
         }
         for (int s = 0; s < LP_STAGES; ++s) {
             mbar_init(smem_u32(&bar_full[s]), 1 + 2 * 4);
@@ -481,19 +536,19 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_consta
         uint32_t issued = 0;
         bool ok = true;
         LinearUnit u;
-        for (int it = 0; ok && linear_unit(p, pair, it, u); ++it) {
+        for (int it = 0; ok && linear_unit<SPLIT>(p, pair, it, u); ++it) {
             if (u.halves == 0) continue;
-            const int b0 = u.tok0 + static_cast<int>(rank) * CTA_ROWS;
+            const int b0 = u.tok0 + static_cast<int>(rank) * (ntile / 2), box_rows = SPLIT ? p.box_rows : TILE_K, boxes = (ntile / 2 + box_rows - 1) / box_rows;
             for (int kb = 0; kb < kblocks; ++kb) {
                 if (!bounded_wait(smem_u32(&bar_empty[s]), ph ^ 1u, wc, 1u, it)) { ok = false; break; }
                 const uint32_t full_local = smem_u32(&bar_full[s]);
-                if (rank == 0) mbar_arrive_expect_tx(full_local, 2 * u.halves * LP_SLOT_BYTES);      // both CTAs' bytes
-                const uint32_t full = map_to_cta(full_local, 0);
+                if (rank == 0) mbar_arrive_expect_tx(full_local, 2 * u.halves * boxes * box_rows * 128);      // both CTAs' bytes
+                const uint32_t full = map_to_cta(full_local, leader);
                 const uint32_t stage = ring + s * LP_STAGE_BYTES;
                 for (int h = 0; h < u.halves; ++h)
-#pragma unroll
-                    for (int q = 0; q < CTA_ROWS / TILE_K; ++q)
-                        tma_load_3d_pair(stage + (1 + h) * LP_SLOT_BYTES + q * BOX_BYTES, &mapX, full, kb * TILE_K, b0 + h * TILE_N + q * TILE_K, 0);
+                    for (int q = 0; q < boxes; ++q)
+                        tma_load_3d_pair(stage + (1 + h) * LP_SLOT_BYTES + q * BOX_BYTES, &mapX, full, (kfirst + kb) * TILE_K, b0 + h * TILE_N + q * TILE_K,
+                                         0);
                 ++issued;
                 if (++s == LP_STAGES) { s = 0; ph ^= 1u; }
             }
@@ -511,21 +566,26 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_consta
         uint32_t ph = 0;
         bool ok = true;
         LinearUnit u;
-        for (int it = 0; ok && linear_unit(p, pair, it, u); ++it) {
+        for (int it = 0; ok && linear_unit<SPLIT>(p, pair, it, u); ++it) {
             if (u.halves == 0) continue;
             const int a0 = u.row0 + static_cast<int>(rank) * CTA_ROWS;
-            for (int kb = 0; kb < kblocks; ++kb) {
+            for (int kb = 0; kb < kblocks; kb += LP_CODE_KSTEPS) {
                 if (!bounded_wait(smem_u32(&bar_codes_used[c]), ph ^ 1u, wc, 7u, it)) { ok = false; break; }
                 const uint32_t bar = smem_u32(&bar_codes[c]);
                 mbar_arrive_expect_tx(bar, LP_CODE_BYTES);
-                tma_load_3d(code_ring + c * LP_CODE_BYTES, &mapC, bar, (BACK ? a0 : kb * TILE_K) >> 1, BACK ? kb * TILE_K : a0, 0);
+                tma_load_3d(code_ring + c * LP_CODE_BYTES, &mapC, bar, (BACK ? a0 : (kfirst + kb) * TILE_K) >> 1, BACK ? (kfirst + kb) * TILE_K : a0,
+                            0);
                 if (++c == LP_CODE_SLOTS) { c = 0; ph ^= 1u; }
             }
         }
         if (!ok) spin_ns(1000000ull);
-    } else if (warp == 3 && lane == 0 && rank == 0) {
+    } else if (warp == 3 && rank == 0) {
         // ------------------------------------------------------------------ MMA issuer (first CTA)
-        const uint32_t idesc = umma_idesc_16(TILE_M, TILE_N, p.bf16 != 0, BACK, false);
+        // The whole warp walks the loop and one lane issues: loop counters and descriptors are then known to be the same for all lanes and live
+        // in uniform registers, from which the instruction takes its operands.  In a branch of one lane they have to be moved there, and
+        // the four products of a k-step took 384 clocks to issue.
+        const bool elected = elect_one();
+        const uint32_t idesc = umma_idesc_16(TILE_M, static_cast<uint32_t>(ntile), p.bf16 != 0, BACK, false);
         int s = 0;
         uint32_t ph = 0;
         uint32_t acc_ph = 0u;                           // bit b: phase of accumulator b
@@ -533,21 +593,23 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_consta
         bool ok = true;
         auto multiply = [&](int stage, int half, uint32_t d_tmem, bool first) {
             const uint32_t sa = ring + stage * LP_STAGE_BYTES, sb = sa + (1 + half) * LP_SLOT_BYTES;
+            const uint64_t adesc = BACK ? umma_smem_desc_mn_sw128(sa, BOX_BYTES, 1024) : umma_smem_desc_k_sw128(sa);
+            const uint64_t bdesc = umma_smem_desc_k_sw128(sb);
+            constexpr uint64_t a_step = (BACK ? 16 * 128 : 32) >> 4, b_step = 32 >> 4;
+            if (elected) {
+                umma_bf16(d_tmem, adesc, bdesc, idesc, first ? 0u : 1u);
 #pragma unroll
-            for (int k16 = 0; k16 < TILE_K / 16; ++k16) {
-                const uint64_t adesc = BACK ? umma_smem_desc_mn_sw128(sa + k16 * 16 * 128, BOX_BYTES, 1024) : umma_smem_desc_k_sw128(sa + k16 * 32);
-                const uint64_t bdesc = umma_smem_desc_k_sw128(sb + k16 * 32);
-                umma_bf16(d_tmem, adesc, bdesc, idesc, (!first || k16 != 0) ? 1u : 0u);
+                for (int k16 = 1; k16 < TILE_K / 16; ++k16) umma_bf16(d_tmem, adesc + k16 * a_step, bdesc + k16 * b_step, idesc, 1u);
             }
         };
         auto acquire = [&](int b, int it) {
-            if (!bounded_wait_hot(smem_u32(&bar_acc_empty[b]), ((acc_ph >> b) & 1u) ^ 1u, wc, 2u, it)) return false;
+            if (!warp_wait_hot(smem_u32(&bar_acc_empty[b]), ((acc_ph >> b) & 1u) ^ 1u, wc, 2u, it)) return false;
             acc_ph ^= 1u << b;
             tc_fence_after_sync();
             return true;
         };
         LinearUnit u;
-        for (int it = 0; ok && linear_unit(p, pair, it, u); ++it) {
+        for (int it = 0; ok && linear_unit<SPLIT>(p, pair, it, u); ++it) {
             if (u.halves == 0) continue;
             const uint32_t d0 = tmem_base + static_cast<uint32_t>(buf * TILE_N), d1 = tmem_base + static_cast<uint32_t>((buf ^ 1) * TILE_N);
             if (!acquire(buf, it)) { ok = false; break; }
@@ -558,7 +620,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_consta
                 int sl = s;
                 uint32_t phl = ph;
                 for (int kb = 0; kb < lead; ++kb) {
-                    if (!bounded_wait_hot(smem_u32(&bar_full[sl]), phl, wc, 3u, it)) { ok = false; break; }
+                    if (!warp_wait_hot(smem_u32(&bar_full[sl]), phl, wc, 3u, it)) { ok = false; break; }
                     tc_fence_after_sync();
                     multiply(sl, 0, d0, kb == 0);
                     if (++sl == LP_STAGES) { sl = 0; phl ^= 1u; }
@@ -567,20 +629,23 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_consta
             }
             for (int kb = 0; kb < kblocks; ++kb) {
                 if (kb >= lead) {
-                    if (!bounded_wait_hot(smem_u32(&bar_full[s]), ph, wc, 3u, it)) { ok = false; break; }
+                    if (!warp_wait_hot(smem_u32(&bar_full[s]), ph, wc, 3u, it)) { ok = false; break; }
                     tc_fence_after_sync();
                     multiply(s, 0, d0, kb == 0);
                 }
-                if (kb == kblocks - 1) umma_commit_pair(smem_u32(&bar_acc_full[buf]));
+                if (kb == kblocks - 1 && elected) umma_commit_pair_at(leader, smem_u32(&bar_acc_full[buf]));
                 if (u.halves == 2) multiply(s, 1, d1, kb == 0);
-                umma_commit_pair(smem_u32(&bar_empty[s]));
+                if (elected) umma_commit_pair_at(leader, smem_u32(&bar_empty[s]));
                 if (++s == LP_STAGES) { s = 0; ph ^= 1u; }
             }
             if (!ok) break;
-            if (u.halves == 2) umma_commit_pair(smem_u32(&bar_acc_full[buf ^ 1]));
-            else buf ^= 1;
+            if (u.halves == 2) {
+                if (elected) umma_commit_pair_at(leader, smem_u32(&bar_acc_full[buf ^ 1]));
+            } else {
+                buf ^= 1;
+            }
         }
-        if (!ok) {
+        if (!ok && elected) {
             // Make sure no MMA is still writing TMEM when it is released.
             umma_commit_local(smem_u32(&bar_drain));
             const uint64_t t0 = global_timer_ns();
@@ -591,7 +656,6 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_consta
         const int grp = (warp - 4) >> 2;                            // takes k-steps grp, grp + LP_LOOK_GROUPS, ... of the launch
         const int r = ((warp - 4) & 3) * 32 + lane;                 // forward: channel; backward: channel r % 64, columns 64 (r / 64) ..
         const uint32_t slot = BACK ? static_cast<uint32_t>((r >> 6) * BOX_BYTES + (r & 63) * 128) : static_cast<uint32_t>(r * 128);
-        const uint32_t code_at = BACK ? static_cast<uint32_t>((r & 63) * 64 + (r >> 6) * 32) : static_cast<uint32_t>(r * 32);
         const uint32_t xor7 = static_cast<uint32_t>(r & 7);
         // Backward: the levels of channel r % 64 of k-step kb, asked for a k-step of the group ahead.
         struct Levels {
@@ -602,66 +666,73 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_consta
             t.a = ld_u32x4(tb);
             t.b = ld_u32x4(tb + 1);
         };
-        LevelPlanes lv;
-        int s = grp, c = grp;
-        uint32_t ph = 0, cph = 0;
-        int kb = grp, it = 0, levels_of = -1;
-        bool ok = true;
-        LinearUnit u;
-        bool valid = linear_unit(p, pair, 0, u);
-        auto settle = [&]() {                                       // into the tile that the k-step lies in
-            while (valid && (u.halves == 0 || kb >= kblocks)) {
-                if (u.halves != 0) kb -= kblocks;
-                valid = linear_unit(p, pair, ++it, u);
+        // 16 bytes q of this thread's 32 bytes of codes for k-step kk of a slot, as the TMA's swizzle left them: forward rows of 128 bytes,
+        // four k-steps; backward rows of 64 bytes, 64 rows a k-step.
+        auto code_at = [&](int kk, int q) {
+            if (BACK) {
+                const uint32_t row = static_cast<uint32_t>(kk * TILE_K + (r & 63));
+                return row * 64 + ((static_cast<uint32_t>((r >> 6) * 2 + q) ^ ((row >> 1) & 3u)) << 4);
             }
+            return static_cast<uint32_t>(r * 128) + ((static_cast<uint32_t>(kk * 2 + q) ^ xor7) << 4);
         };
-        settle();
-        Levels ahead{};
-        if (BACK && valid) levels_at(kb * TILE_K + (r & 63), ahead);
-        // Every lane waits through lane 0, then observes the completed phase itself.
-        auto wait = [&](uint32_t bar, uint32_t parity, uint32_t site) {
+        // All lanes look, and only a warp that has to wait does so through lane 0: with that branch in every step (two a step, and the
+        // votes around it) 32 tokens of 28672 -> 8192 took 133 us instead of 108, 8192 tokens of 4096 x 4096 224 instead of 206.
+        auto wait = [&](uint32_t bar, uint32_t parity, uint32_t site, int it) {
+            if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
             bool got = true;
             if (lane == 0) got = bounded_wait(bar, parity, wc, site, it);
             got = __any_sync(0xffffffffu, got && lane == 0);
-            if (got) (void)mbar_try_wait(bar, parity);
+            if (got) (void)mbar_try_wait(bar, parity);       // every lane observes the completed phase
             return got;
         };
-        while (valid) {
-            if (BACK) {
-                lv.set(ahead.a, ahead.b);
-                int kn = kb + LP_LOOK_GROUPS;                       // (past the last tile: some channel's levels, not used)
-                while (kn >= kblocks) kn -= kblocks;
-                levels_at(kn * TILE_K + (r & 63), ahead);
-            } else if (levels_of != it) {
-                levels_of = it;
-                levels_at(u.row0 + static_cast<int>(rank) * CTA_ROWS + r, ahead);
-                lv.set(ahead.a, ahead.b);
-            }
-            if (!wait(smem_u32(&bar_codes[c]), cph, 6u)) { ok = false; break; }
-            const uint4 c0 = ld_shared_16(code_ring + c * LP_CODE_BYTES + code_at), c1 = ld_shared_16(code_ring + c * LP_CODE_BYTES + code_at + 16);
-            if (!wait(smem_u32(&bar_empty[s]), ph ^ 1u, 8u)) { ok = false; break; }
-            const uint32_t base = ring + s * LP_STAGE_BYTES + slot;
-            // the last, ragged k-step: no level meets padding (infinite ones would make it NaN)
-            const int end = BACK ? p.d_out - (kb * TILE_K + (r & 63)) > 0 ? TILE_K : 0 : p.d_in - kb * TILE_K;
-            const uint32_t w[8] = {c0.x, c0.y, c0.z, c0.w, c1.x, c1.y, c1.z, c1.w};
+        LevelPlanes lv;
+        uint32_t done = 0, slots = 0;                               // k-steps and code slots of the tiles before
+        bool ok = true;
+        LinearUnit u;
+        for (int it = 0; ok && linear_unit<SPLIT>(p, pair, it, u); ++it) {
+            if (u.halves == 0) continue;
+            Levels ahead{};
+            levels_at(BACK ? (kfirst + grp) * TILE_K + (r & 63) : u.row0 + static_cast<int>(rank) * CTA_ROWS + r, ahead);
+            if (!BACK) lv.set(ahead.a, ahead.b);
+            for (int k4 = 0; ok && k4 < kblocks; k4 += LP_CODE_KSTEPS, ++slots) {
+                const uint32_t c = slots % LP_CODE_SLOTS, codes = code_ring + c * LP_CODE_BYTES;
+                if (!wait(smem_u32(&bar_codes[c]), (slots / LP_CODE_SLOTS) & 1u, 6u, it)) { ok = false; break; }
+                uint4 code[LP_CODE_KSTEPS / LP_LOOK_GROUPS][2];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                uint4 v = lv.look<WIDE>(w[e]);
-                if (8 * e >= end) v = make_uint4(0u, 0u, 0u, 0u);
-                st_shared_16(base + ((static_cast<uint32_t>(e) ^ xor7) << 4), v);
+                for (int i = 0; i < LP_CODE_KSTEPS / LP_LOOK_GROUPS; ++i)
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) code[i][q] = ld_shared_16(codes + code_at(LP_LOOK_GROUPS * i + grp, q));
+#pragma unroll
+                for (int i = 0; i < LP_CODE_KSTEPS / LP_LOOK_GROUPS; ++i) {
+                    const int kb = k4 + LP_LOOK_GROUPS * i + grp;
+                    if (kb >= kblocks) break;
+                    if (BACK) {
+                        lv.set(ahead.a, ahead.b);
+                        levels_at((kfirst + kb + LP_LOOK_GROUPS) * TILE_K + (r & 63), ahead);
+                    }
+                    const uint32_t step = done + static_cast<uint32_t>(kb), s = step % LP_STAGES;
+                    if (!wait(smem_u32(&bar_empty[s]), ((step / LP_STAGES) & 1u) ^ 1u, 8u, it)) { ok = false; break; }
+                    const uint32_t base = ring + s * LP_STAGE_BYTES + slot;
+                    const uint32_t w[8] = {code[i][0].x, code[i][0].y, code[i][0].z, code[i][0].w, code[i][1].x, code[i][1].y, code[i][1].z, code[i][1].w};
+                    const int left = kdim - (kfirst + kb) * TILE_K;
+                    if (left >= TILE_K) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) st_shared_16(base + ((static_cast<uint32_t>(e) ^ xor7) << 4), lv.look<WIDE>(w[e]));
+                    } else {
+                        // the last, ragged k-step: no level meets padding (infinite ones would make it NaN)
+                        const int end = BACK ? ((r & 63) < left ? TILE_K : 0) : left;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            st_shared_16(base + ((static_cast<uint32_t>(e) ^ xor7) << 4), 8 * e < end ? lv.look<WIDE>(w[e]) : make_uint4(0u, 0u, 0u, 0u));
+                    }
+                    fence_proxy_async_smem();        // make the stores visible to the tensor core's reads
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_cluster(map_to_cta(smem_u32(&bar_full[s]), leader));
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&bar_codes_used[c]));
             }
-            fence_proxy_async_smem();                // make the stores visible to the tensor core's reads
-            __syncwarp();
-            if (lane == 0) {
-                mbar_arrive_cluster(map_to_cta(smem_u32(&bar_full[s]), 0));
-                mbar_arrive(smem_u32(&bar_codes_used[c]));
-            }
-            s += LP_LOOK_GROUPS;
-            if (s >= LP_STAGES) { s -= LP_STAGES; ph ^= 1u; }
-            c += LP_LOOK_GROUPS;
-            if (c >= LP_CODE_SLOTS) { c -= LP_CODE_SLOTS; cph ^= 1u; }
-            kb += LP_LOOK_GROUPS;
-            settle();
+            done += static_cast<uint32_t>(kblocks);
         }
         (void)ok;
     } else if (warp >= 4 + LP_LOOK_WARPS) {
@@ -676,7 +747,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_consta
         int buf = 0;
         bool ok = true;
         LinearUnit u;
-        for (int it = 0; ok && linear_unit(p, pair, it, u); ++it) {
+        for (int it = 0; ok && linear_unit<SPLIT>(p, pair, it, u); ++it) {
             const int row = u.row0 + static_cast<int>(rank) * CTA_ROWS + q * 32 + lane;
             const bool in = row < rows;
             float bias = 0.0f;
@@ -694,12 +765,20 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_consta
 #pragma unroll 1
                 for (int n0 = 0; n0 < 128; n0 += 32) {
                     uint32_t acc[32];
+                    if (SPLIT && part * 128 + n0 >= ntile) break;
                     tmem_ld_32x32(tmem_tile + static_cast<uint32_t>(n0), acc);
                     tmem_ld_wait();
+                    if (SPLIT) {
+                        // partial sums [token][row], where the ring was: all its stages have been used
+                        const uint32_t at = ring + static_cast<uint32_t>(((part * 128 + n0) * CTA_ROWS + q * 32 + lane) * 4);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) st_shared_4(at + e * CTA_ROWS * 4, acc[e]);
+                        continue;
+                    }
                     if (n0 == 96) {
                         tc_fence_before_sync();
                         __syncwarp();
-                        if (lane == 0) mbar_arrive_cluster(map_to_cta(smem_u32(&bar_acc_empty[buf]), 0));
+                        if (lane == 0) mbar_arrive_cluster(map_to_cta(smem_u32(&bar_acc_empty[buf]), leader));
                     }
                     const int left = in ? p.n - static_cast<int>(tok0) - n0 : 0;       // this lane's tokens 0, 2, ... below it exist
                     float2 v[16];
@@ -752,6 +831,44 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_consta
         }
     }
 
+    if (SPLIT) {
+        __syncwarp();
+        cluster_sync_all();                             // all partial sums are there
+        LinearUnit u;
+        (void)linear_unit<SPLIT>(p, pair, 0, u);
+        const bool bf16 = p.bf16 != 0;
+        const int t0 = ntile * share / p.ranks, t1 = ntile * (share + 1) / p.ranks, row = u.row0 + static_cast<int>(rank) * CTA_ROWS + lane * 4;
+        // a warp takes a token, a lane four rows (rows come in eights)
+        for (int t = t0 + warp; t < t1; t += LP_THREADS / 32) {
+            const long long token = u.tok0 + t;
+            if (token >= p.n || row >= rows) continue;
+            float v[4] = {0.f, 0.f, 0.f, 0.f};
+            for (int r = 0; r < p.ranks; ++r) {
+                float part[4];
+                ld_cluster_f32x4(map_to_cta(ring + static_cast<uint32_t>((t * CTA_ROWS + lane * 4) * 4), 2 * r + rank), part);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] += part[e];
+            }
+            if (!BACK) {
+                if (p.bias) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] += half_value(ld_u16(p.bias + row + e), bf16);
+                }
+                if (p.Z) *reinterpret_cast<uint2 *>(p.Z + token * p.ld_z + row) = make_uint2(half2_bits(v[0], v[1], bf16), half2_bits(v[2], v[3], bf16));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = activate(v[e], p.act);
+                if (p.residual) {
+                    const uint2 res = ld_u32x2(p.residual + token * p.ld_r + row);
+                    const float2 a = half2_value(res.x, bf16), b = half2_value(res.y, bf16);
+                    v[0] += a.x;
+                    v[1] += a.y;
+                    v[2] += b.x;
+                    v[3] += b.y;
+                }
+            }
+            *reinterpret_cast<uint2 *>(p.out + token * p.ld_out + row) = make_uint2(half2_bits(v[0], v[1], bf16), half2_bits(v[2], v[3], bf16));
+        }
+    }
     __syncwarp();
     tc_fence_before_sync();
     cluster_sync_all();
