@@ -1382,10 +1382,12 @@ int32_t gq_token_logprobs(const void *logits, int32_t dtype, int64_t n, int64_t 
     if (int32_t rc = check_disjoint(wr, ro)) return rc;
     DeviceInfo *di;
     if (int32_t rc = device_info(&di)) return rc;
-    // Rows are split while there are fewer CTAs than SMs and a CTA keeps a round of 16-byte loads.
+    // Rows for eight CTAs of 128 threads on every SM: such CTAs, one a row.  Otherwise 512 threads, and rows are split while there are fewer
+    // CTAs than SMs and a CTA keeps a round of 16-byte loads.
+    const bool narrow = n >= 8 * static_cast<int64_t>(di->sm_count);
     unsigned ranks = 1;
     const int64_t chunks = vocab * static_cast<int64_t>(dtype_bytes(dtype)) / 16;
-    while (ranks < gq::SC_MAX_CLUSTER && n * ranks < di->sm_count && chunks >= 2 * ranks * gq::SC_THREADS) ranks *= 2;
+    while (!narrow && ranks < gq::SC_MAX_CLUSTER && n * ranks < di->sm_count && chunks >= 2 * ranks * gq::SC_WIDE) ranks *= 2;
     gq::ScoreParams p{};
     p.logits = logits;
     p.ld = ld;
@@ -1400,9 +1402,12 @@ int32_t gq_token_logprobs(const void *logits, int32_t dtype, int64_t n, int64_t 
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     {
         LaunchScope scope(GQ_KERNEL_SCORE, st);
-        const auto kernel = dtype == GQ_DTYPE_BF16 ? gq::token_logprobs_kernel<0> : dtype == GQ_DTYPE_FP16 ? gq::token_logprobs_kernel<1>
-                                                                                                      : gq::token_logprobs_kernel<2>;
-        launch_cluster(kernel, ranks, dim3(static_cast<unsigned>(n) * ranks), gq::SC_THREADS, 0, st, p, static_cast<int>(ranks));
+        const auto wide = dtype == GQ_DTYPE_BF16 ? gq::token_logprobs_kernel<0, gq::SC_WIDE>
+                        : dtype == GQ_DTYPE_FP16 ? gq::token_logprobs_kernel<1, gq::SC_WIDE> : gq::token_logprobs_kernel<2, gq::SC_WIDE>;
+        const auto many = dtype == GQ_DTYPE_BF16 ? gq::token_logprobs_kernel<0, gq::SC_NARROW>
+                        : dtype == GQ_DTYPE_FP16 ? gq::token_logprobs_kernel<1, gq::SC_NARROW> : gq::token_logprobs_kernel<2, gq::SC_NARROW>;
+        launch_cluster(narrow ? many : wide, ranks, dim3(static_cast<unsigned>(n) * ranks), narrow ? gq::SC_NARROW : gq::SC_WIDE, 0, st, p,
+                       static_cast<int>(ranks));
     }
     GQ_CUDA(cudaGetLastError());
     return GQ_OK;

@@ -18,8 +18,9 @@
 
 namespace gq {
 
-constexpr int SC_THREADS = 512;
-constexpr int SC_WARPS = SC_THREADS / 32;
+constexpr int SC_WIDE = 512;             // threads of a CTA where rows are few
+constexpr int SC_NARROW = 128;           // and where there are many
+constexpr int SC_GROUPS = 64;            // groups of threads whose largest values bound the alternatives from below
 constexpr int SC_MAX_TOP = 32;
 constexpr int SC_MAX_CLUSTER = 8;
 constexpr int SC_CANDIDATES = 256;       // entries that may reach the highest alternatives of a CTA's part of a row
@@ -83,6 +84,37 @@ struct LogitRow {
             f[3] = __uint_as_float(v.w);
         }
     }
+    // The largest number among four chunks and `top`.  16-bit types in pairs: half the instructions.
+    static __device__ __forceinline__ float largest(const uint4 (&v)[4], float top)
+    {
+        if constexpr (DT == 2) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                top = fmaxf(fmaxf(fmaxf(top, __uint_as_float(v[q].x)), __uint_as_float(v[q].y)), fmaxf(__uint_as_float(v[q].z), __uint_as_float(v[q].w)));
+            return top;
+        } else {
+            uint32_t m = pair_max(pair_max(v[0].x, v[0].y), pair_max(v[0].z, v[0].w));
+#pragma unroll
+            for (int q = 1; q < 4; ++q) m = pair_max(m, pair_max(pair_max(v[q].x, v[q].y), pair_max(v[q].z, v[q].w)));
+            float lo, hi;
+            if constexpr (DT == 0) {
+                lo = __uint_as_float(m << 16);
+                hi = __uint_as_float(m & 0xffff0000u);
+            } else {
+                const float2 t = __half22float2(*reinterpret_cast<const __half2 *>(&m));
+                lo = t.x;
+                hi = t.y;
+            }
+            return fmaxf(top, fmaxf(lo, hi));
+        }
+    }
+    static __device__ __forceinline__ uint32_t pair_max(uint32_t a, uint32_t b)
+    {
+        uint32_t r;
+        if constexpr (DT == 0) asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+        else asm("max.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+        return r;
+    }
 };
 
 // Running softmax statistics: maximum, sum of 2^y and of y 2^y with y = (x - max) log2 e.  The maximum starts at the lowest
@@ -140,23 +172,22 @@ __device__ __forceinline__ unsigned long long warp_highest(unsigned long long v)
     return (static_cast<unsigned long long>(key) << 32) | low;
 }
 
-// One warp: the `top` highest of `count` <= SC_CANDIDATES entries, in order, into out (0 where there are no more).
-__device__ __forceinline__ void warp_select(const unsigned long long *entries, int count, int top, unsigned long long *out)
+// The whole CTA: the `top` highest of `count` <= SC_CANDIDATES entries, in order, into out (0 where there are no more).  An entry's place
+// is the number of entries above it; all are different but for the zeros.
+template <int THREADS>
+__device__ __forceinline__ void block_select(const unsigned long long *entries, int count, int top, unsigned long long *out)
 {
-    const int lane = threadIdx.x & 31;
-    unsigned long long v[SC_CANDIDATES / 32];
-#pragma unroll
-    for (int q = 0; q < SC_CANDIDATES / 32; ++q) v[q] = lane + 32 * q < count ? entries[lane + 32 * q] : 0ull;
-    for (int r = 0; r < top; ++r) {
-        unsigned long long best = v[0];
-#pragma unroll
-        for (int q = 1; q < SC_CANDIDATES / 32; ++q) best = v[q] > best ? v[q] : best;
-        best = warp_highest(best);
-        if (lane == 0) out[r] = best;
-#pragma unroll
-        for (int q = 0; q < SC_CANDIDATES / 32; ++q)
-            if (v[q] == best) v[q] = 0ull;
+    const int tid = threadIdx.x;
+    if (tid < top) out[tid] = 0ull;
+    __syncthreads();
+    for (int q = tid; q < count; q += THREADS) {
+        const unsigned long long mine = entries[q];
+        int above = 0;
+#pragma unroll 8
+        for (int j = 0; j < count; ++j) above += entries[j] > mine ? 1 : 0;
+        if (mine != 0ull && above < top) out[above] = mine;
     }
+    __syncthreads();
 }
 
 struct ScoreParams {
@@ -184,18 +215,23 @@ __device__ __forceinline__ unsigned long long ld_cluster_u64(uint32_t addr)
 // One cluster of `ranks` CTAs per row, each CTA a contiguous part of the row's chunks: one CTA where there are rows enough for
 // all SMs, up to eight where there are few.  The first CTA joins the parts through distributed shared memory.
 //
-// Alternatives: a thread keeps only the largest of its values.  The top-th largest of these is a value that at least `top`
-// entries reach, so every alternative is among the entries not below it, and those are with the threads whose largest is not
-// below it: about `top` threads, whose chunks are read again (from L2) by their warp, 32 chunks at a time.  What is found
-// there, hardly more than `top` entries, is sorted out by one warp.  Where ties make more than SC_CANDIDATES of them (a row of
-// equal logits), the row is gone through once for each alternative instead.
-template <int DT>
-__global__ void __launch_bounds__(SC_THREADS) token_logprobs_kernel(const ScoreParams p, int ranks)
+// Alternatives: a thread keeps only the largest of its values.  Of 64 groups of threads, the top-th largest of the groups' largest
+// values is one that at least `top` entries reach, so every alternative is among the entries not below it, and those are with the
+// threads whose largest is not below it: about `top` threads, whose chunks are read again (from L2) by their warp, 32 chunks at a
+// time.  What is found there, hardly more than `top` entries, is put in order by counting who is above whom.  Where ties make more than SC_CANDIDATES of
+// them (a row of equal logits), the row is gone through once for each alternative instead.
+//
+// Many rows: CTAs of 128 threads, so that an SM works on many rows at once and the joints between a row's end and the next one's
+// beginning are covered; 4096 x 32000 bf16 took 80 us with 512 threads a row.
+template <int DT, int THREADS>
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS) token_logprobs_kernel(const ScoreParams p, int ranks)
 {
     using Row = LogitRow<DT>;
-    __shared__ float red[3][SC_WARPS];
+    constexpr int WARPS = THREADS / 32;
+    __shared__ float red[3][WARPS];
     __shared__ float part[3];                                     // this CTA's statistics
-    __shared__ float best_of[SC_THREADS];
+    __shared__ uint32_t best_of[THREADS];
+    __shared__ uint32_t group_best[SC_GROUPS];
     __shared__ unsigned long long found[SC_CANDIDATES];
     __shared__ unsigned long long chosen[SC_MAX_TOP];             // this CTA's alternatives
     __shared__ uint32_t floor_key;
@@ -216,44 +252,51 @@ __global__ void __launch_bounds__(SC_THREADS) token_logprobs_kernel(const ScoreP
 
     SoftStats st{-FLT_MAX, 0.0f, 0.0f};
     float best = __uint_as_float(0xff800000u);                    // -inf
-    auto take = [&](const uint4 (&v)[4], int count) {
-        float f[4][Row::PER];
-        float top = best;
+    auto take = [&](const uint4 (&v)[4]) {
+        best = Row::largest(v, best);
+        if (best > st.m) st.raise(best);
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            if (q >= count) break;
-            Row::unpack(v[q], f[q]);
+            float f[Row::PER];
+            Row::unpack(v[q], f);
 #pragma unroll
-            for (int e = 0; e < Row::PER; ++e) top = fmaxf(top, f[q][e]);
-        }
-        best = top;
-        if (top > st.m) st.raise(top);
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            if (q >= count) break;
-#pragma unroll
-            for (int e = 0; e < Row::PER; ++e) st.add(f[q][e]);
+            for (int e = 0; e < Row::PER; ++e) st.add(f[e]);
         }
     };
+    // Four chunks at a time, the next four on their way while four are added up.
     int c = c0 + tid;
-    for (; c + 3 * SC_THREADS < c1; c += 4 * SC_THREADS) {
-        uint4 v[4];
+    const int rounds = c < c1 ? (c1 - c + THREADS - 1) / THREADS : 0;       // chunks of this thread
+    auto load = [&](uint4 (&v)[4]) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) v[q] = ld_once_16(row.chunk(c + q * SC_THREADS));
-        take(v, 4);
+        for (int q = 0; q < 4; ++q) v[q] = ld_once_16(row.chunk(c + q * THREADS));
+        c += 4 * THREADS;
+    };
+    int left = rounds;
+    if (left >= 4) {
+        uint4 v[4], w[4];
+        load(v);
+        for (left -= 4; left >= 8; left -= 8) {
+            load(w);
+            take(v);
+            load(v);
+            take(w);
+        }
+        if (left >= 4) {
+            load(w);
+            take(v);
+            take(w);
+            left -= 4;
+        } else {
+            take(v);
+        }
     }
-    {
+    if (left > 0) {
+        // the last ones; what is not there is -inf, which adds nothing
+        const uint32_t none = DT == 0 ? 0xff80ff80u : DT == 1 ? 0xfc00fc00u : 0xff800000u;
         uint4 v[4];
-        int count = 0;
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-            if (c + q * SC_THREADS < c1) {
-                v[q] = ld_once_16(row.chunk(c + q * SC_THREADS));
-                count = q + 1;
-            } else {
-                v[q] = make_uint4(0u, 0u, 0u, 0u);
-            }
-        if (count) take(v, count);
+        for (int q = 0; q < 4; ++q) v[q] = q < left ? ld_once_16(row.chunk(c + q * THREADS)) : make_uint4(none, none, none, none);
+        take(v);
     }
     if (extra >= 0) {
         const float x = row.at(extra);
@@ -263,7 +306,7 @@ __global__ void __launch_bounds__(SC_THREADS) token_logprobs_kernel(const ScoreP
     }
 
     const bool alternatives = p.top > 0;
-    if (alternatives) best_of[tid] = best;
+    if (alternatives) best_of[tid] = value_key(best);
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) {
         SoftStats o;
@@ -280,9 +323,9 @@ __global__ void __launch_bounds__(SC_THREADS) token_logprobs_kernel(const ScoreP
     __syncthreads();
     if (warp == 0) {
         SoftStats w{-FLT_MAX, 0.0f, 0.0f};
-        if (lane < SC_WARPS) w = SoftStats{red[0][lane], red[1][lane], red[2][lane]};
+        if (lane < WARPS) w = SoftStats{red[0][lane], red[1][lane], red[2][lane]};
 #pragma unroll
-        for (int off = SC_WARPS / 2; off > 0; off >>= 1) {
+        for (int off = WARPS / 2; off > 0; off >>= 1) {
             SoftStats o;
             o.m = __shfl_xor_sync(0xffffffffu, w.m, off);
             o.s = __shfl_xor_sync(0xffffffffu, w.s, off);
@@ -295,28 +338,25 @@ __global__ void __launch_bounds__(SC_THREADS) token_logprobs_kernel(const ScoreP
             part[2] = w.t;
         }
     } else if (warp == 1 && alternatives) {
-        // the top-th largest of the threads' largest values
-        uint32_t k[SC_WARPS];
+        // the largest value that at least `top` of the groups reach
+        uint32_t mine[2];
 #pragma unroll
-        for (int q = 0; q < SC_WARPS; ++q) k[q] = value_key(best_of[lane + 32 * q]);
-        uint32_t highest = 0u;
-        for (int r = 0; r < p.top; ++r) {
-            uint32_t b = k[0];
+        for (int h = 0; h < 2; ++h) {
+            uint32_t k = 0u;
 #pragma unroll
-            for (int q = 1; q < SC_WARPS; ++q) b = max(b, k[q]);
-            highest = __reduce_max_sync(0xffffffffu, b);
-            const uint32_t holders = __ballot_sync(0xffffffffu, b == highest);
-            if (lane == __ffs(holders) - 1) {            // taken once, by the first lane that has it
-                bool done = false;
-#pragma unroll
-                for (int q = 0; q < SC_WARPS; ++q)
-                    if (!done && k[q] == highest) {
-                        k[q] = 0u;
-                        done = true;
-                    }
-            }
+            for (int q = 0; q < THREADS / SC_GROUPS; ++q) k = max(k, best_of[h * 32 + lane + q * SC_GROUPS]);
+            mine[h] = group_best[h * 32 + lane] = k;
         }
-        if (lane == 0) floor_key = highest;
+        __syncwarp();
+        int reach[2] = {0, 0};
+#pragma unroll 8
+        for (int j = 0; j < SC_GROUPS; ++j) {
+            const uint32_t k = group_best[j];
+            reach[0] += k >= mine[0] ? 1 : 0;
+            reach[1] += k >= mine[1] ? 1 : 0;
+        }
+        const uint32_t least = __reduce_max_sync(0xffffffffu, max(reach[0] >= p.top ? mine[0] : 0u, reach[1] >= p.top ? mine[1] : 0u));
+        if (lane == 0) floor_key = least;
     }
 
     if (alternatives) {
@@ -333,7 +373,7 @@ __global__ void __launch_bounds__(SC_THREADS) token_logprobs_kernel(const ScoreP
             const int owner = __ffs(hot) - 1;
             hot &= hot - 1;
             const int first = c0 + warp * 32 + owner;
-            for (int i = first + lane * SC_THREADS; i < c1; i += 32 * SC_THREADS) {
+            for (int i = first + lane * THREADS; i < c1; i += 32 * THREADS) {
                 float f[Row::PER];
                 Row::unpack(ld_once_16(row.chunk(i)), f);
 #pragma unroll
@@ -344,7 +384,7 @@ __global__ void __launch_bounds__(SC_THREADS) token_logprobs_kernel(const ScoreP
         __syncthreads();
         const int count = n_found;
         if (count <= SC_CANDIDATES) {
-            if (warp == 0) warp_select(found, count, p.top, chosen);
+            block_select<THREADS>(found, count, p.top, chosen);
         } else {
             // ties: the next in order, over the whole part, once per alternative
             unsigned long long last = ~0ull;
@@ -354,7 +394,7 @@ __global__ void __launch_bounds__(SC_THREADS) token_logprobs_kernel(const ScoreP
                     const unsigned long long v = entry_of(x, j);
                     if (v < last && v > high) high = v;
                 };
-                for (int i = c0 + tid; i < c1; i += SC_THREADS) {
+                for (int i = c0 + tid; i < c1; i += THREADS) {
                     float f[Row::PER];
                     Row::unpack(ld_once_16(row.chunk(i)), f);
 #pragma unroll
@@ -365,15 +405,23 @@ __global__ void __launch_bounds__(SC_THREADS) token_logprobs_kernel(const ScoreP
                 __syncthreads();
                 if (lane == 0) found[warp] = high;
                 __syncthreads();
-                for (int q = 0; q < SC_WARPS; ++q) high = found[q] > high ? found[q] : high;
+                for (int q = 0; q < WARPS; ++q) high = found[q] > high ? found[q] : high;
                 last = high;
                 if (tid == 0) chosen[r] = high;
             }
+            __syncthreads();
         }
-        __syncthreads();
     }
 
     if (ranks > 1) cluster_sync_all();
+    if (alternatives && ranks > 1 && rank == 0) {
+        for (int i = tid; i < ranks * p.top; i += THREADS) {
+            const int r = i / p.top;
+            found[i] = ld_cluster_u64(map_to_cta(smem_u32(chosen), r) + 8u * static_cast<uint32_t>(i - r * p.top));
+        }
+        __syncthreads();
+        block_select<THREADS>(found, ranks * p.top, p.top, chosen);
+    }
     if (rank == 0 && warp == 0) {
         __syncwarp();
         SoftStats w{-FLT_MAX, 0.0f, 0.0f};
@@ -405,15 +453,6 @@ __global__ void __launch_bounds__(SC_THREADS) token_logprobs_kernel(const ScoreP
             }
         }
         if (alternatives) {
-            if (ranks > 1) {
-                for (int i = lane; i < ranks * p.top; i += 32) {
-                    const int r = i / p.top;
-                    found[i] = ld_cluster_u64(map_to_cta(smem_u32(chosen), r) + 8u * static_cast<uint32_t>(i - r * p.top));
-                }
-                __syncwarp();
-                warp_select(found, ranks * p.top, p.top, chosen);
-            }
-            __syncwarp();
             if (lane < p.top) {
                 const unsigned long long v = chosen[lane];
                 const float x = key_value(static_cast<uint32_t>(v >> 32));

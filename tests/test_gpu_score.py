@@ -72,7 +72,8 @@ def check_scores(x, t, top):
 
 @pytest.mark.parametrize("dtype", sorted(DT))
 @pytest.mark.parametrize("n,vocab,top", [(1, 1, 1), (2, 2, 2), (3, 7, 7), (2, 8, 3), (5, 9, 0), (1, 511, 32), (3, 512, 1), (2, 4095, 20), (1, 32000, 5),
-                                         (7, 32000, 20), (300, 1000, 4), (150, 50001, 32), (1, 160000, 32), (33, 8200, 2)])
+                                         (7, 32000, 20), (300, 1000, 4), (150, 50001, 32), (1, 160000, 32), (33, 8200, 2), (1200, 33, 32), (1300, 4099, 5),
+                                         (1190, 9000, 32), (1184, 64, 0)])
 def test_scores_match_64_bits(dev, dtype, n, vocab, top):
     x, t, _ = make(dev, n, vocab, DT[dtype], seed=n + vocab)
     check_scores(x, t, top)
@@ -93,6 +94,8 @@ def test_rows_of_equal_logits_give_the_first_indices(dev, dtype):
     x[2] = 0.0
     x[2, 1::2] = -0.0                                     # both zeros are one value
     check_scores(x, torch.tensor([0, 1, 9000], device=dev), 32)
+    x = x.repeat(400, 1)                                  # rows for a CTA of the smaller size each
+    check_scores(x, torch.arange(1200, device=dev) * 7, 32)
 
 
 @pytest.mark.parametrize("dtype", sorted(DT))
@@ -117,6 +120,7 @@ def test_masked_logits(dev, dtype):
     t[2] = int((x[2] == -INF).nonzero()[0])               # a ruled-out target
     t[1], t[4], t[6] = 0, 3, 5002
     for top in (0, 1, 5, 32):
+        check_scores(x.repeat(150, 1), t.repeat(150), top)              # rows for a CTA of the smaller size each
         logp, entropy, stats = check_scores(x, t, top)
     assert stats[0].tolist() == [-INF, 0.0] and entropy[0] == 0 and logp[0] == -INF
     assert logp[1] == 0 and logp[2] == -INF
