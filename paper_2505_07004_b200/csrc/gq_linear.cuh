@@ -50,6 +50,18 @@ __device__ __forceinline__ uint4 ld_shared_16(uint32_t addr)
     return v;
 }
 
+// Asynchronous copies of 16 bytes from global to shared memory, past L1.
+__device__ __forceinline__ void copy_async_16(uint32_t dst, const void *src)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT>
+__device__ __forceinline__ void copy_async_wait()
+{
+    asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory");
+}
+
 // The levels of a channel as byte planes.
 struct LevelPlanes {
     uint32_t lo[4], hi[4];
@@ -179,13 +191,13 @@ struct LinearParams {
 constexpr int LT_WARPS = 8;
 constexpr int LT_THREADS = 32 * LT_WARPS;         // a thread per pair of codes when the tables are built
 constexpr int LT_CHANNELS = 16;
-constexpr int LT_TOKENS = 8;
+constexpr int LT_TOKENS = 8;              // columns of a product; a CTA takes up to two of them
 constexpr int LT_K = 128;                 // contraction indices a warp takes at a time: 32 per lane of a quad
 constexpr int LT_MAX_CLUSTER = 8;
-constexpr int LT_AHEAD = 4;               // a multiple of LT_X_AHEAD
-constexpr int LT_X_AHEAD = 2;
+constexpr int LT_AHEAD = 4;               // pieces of codes on their way to a warp
 constexpr int LT_TABLE_BYTES = 256 * 128;         // levels of all pairs of codes for 8 channels, a word per lane
-constexpr int LT_SMEM_BYTES = 2 * LT_TABLE_BYTES + 32768;      // the tables start at a multiple of their size
+constexpr int LT_CODE_BYTES = 2 * 32 * 16;        // a piece of a warp's codes
+constexpr int LT_SMEM_BYTES = 2 * LT_TABLE_BYTES + LT_WARPS * LT_AHEAD * LT_CODE_BYTES;
 
 template <bool BF16>
 __device__ __forceinline__ void mma_m16n8k16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
@@ -208,56 +220,69 @@ __device__ __forceinline__ void mma_m16n8k16(float (&c)[4], uint32_t a0, uint32_
 // Lookups: a byte of codes names two levels, which stand side by side in a table of 256 words for the channel.  Every lane has its
 // own copy in its own bank (row = byte, word = lane: 32 KB for 8 channels), so 32 random bytes meet no conflicts: a load and two integer
 // instructions for two weights, where looking them up in registers takes more than five.
-template <bool BF16>
+template <bool BF16, int NT>
 __global__ void __launch_bounds__(LT_THREADS, 2) linear_token_kernel(const LinearParams p, int ranks)
 {
-    extern __shared__ uint8_t smem_raw[];
-    __shared__ float sums[LT_WARPS][LT_TOKENS][LT_CHANNELS];
-    __shared__ float mine[LT_TOKENS * LT_CHANNELS];
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
+    constexpr int TOKENS = NT * LT_TOKENS, X_AHEAD = 2 / NT;      // (pieces of activations in registers)
+    __shared__ float sums[LT_WARPS][TOKENS][LT_CHANNELS];
+    __shared__ float mine[TOKENS * LT_CHANNELS];
     __shared__ uint16_t levels[LT_CHANNELS][LIN_LEVELS];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
     const int group = static_cast<int>(blockIdx.x) / ranks, rank = static_cast<int>(blockIdx.x) - group * ranks;
     const int j0 = group * LT_CHANNELS;
-    const uint32_t tables = (smem_u32(smem_raw) + 32767u) & ~32767u;
+    const uint32_t tables = smem_u32(smem_raw), ring = tables + 2 * LT_TABLE_BYTES + static_cast<uint32_t>(warp * LT_AHEAD * LT_CODE_BYTES + lane * 16);
     griddep_launch();
     griddep_wait();
     // channels are a multiple of 8, so either all of g or all of g + 8 are there
     const bool second = j0 + 8 < p.d_out;
     const int ja = j0 + g, jb = second ? ja + 8 : ja;
     const uint8_t *ca = p.codes + static_cast<size_t>(ja) * p.ld_codes, *cb = p.codes + static_cast<size_t>(jb) * p.ld_codes;
-    const uint16_t *x = p.X + static_cast<long long>(g < p.n ? g : 0) * p.ld_x;
-    const bool have = g < p.n;
+    const uint16_t *x[NT];
+    bool have[NT];
+#pragma unroll
+    for (int o = 0; o < NT; ++o) {
+        have[o] = g + o * LT_TOKENS < p.n;
+        x[o] = p.X + static_cast<long long>(have[o] ? g + o * LT_TOKENS : 0) * p.ld_x;
+    }
     const int pieces = (p.d_in + LT_K - 1) / LT_K, stride = ranks * LT_WARPS;
     // A warp's pieces are rank * LT_WARPS + warp, + stride, ...; the `whole` first of them lie inside the row, one ragged piece may follow.
-    // Codes are asked for LT_AHEAD pieces ahead (they come from device memory), activations LT_X_AHEAD (from L2 or L1).
+    // Codes come from device memory, by asynchronous copies LT_AHEAD pieces ahead: each lane copies and reads its own 16 bytes, so nothing but
+    // its own wait is needed; in registers the loads of four pieces shared the few scoreboards there are, and waits for one waited
+    // for the others.  Activations come from L2 or L1, one or two pieces ahead, in registers.
     const int first = rank * LT_WARPS + warp, full = p.d_in / LT_K;
     const int whole = first < full ? (full - first + stride - 1) / stride : 0;
     const bool ragged = full < pieces && full % stride == first;
     const uint8_t *qa = ca + (first * LT_K + 32 * t) / 2, *qb = cb + (first * LT_K + 32 * t) / 2;
-    const uint16_t *xt = x + first * LT_K + 32 * t;
+    size_t xt = static_cast<size_t>(first) * LT_K + 32 * t;
     const size_t code_step = static_cast<size_t>(stride) * LT_K / 2, x_step = static_cast<size_t>(stride) * LT_K;
-    uint4 codes[LT_AHEAD][2], tokens[LT_X_AHEAD][4];
+    uint4 tokens[X_AHEAD][NT][4];
 #pragma unroll
-    for (int d = 0; d < LT_X_AHEAD; ++d)
+    for (int d = 0; d < X_AHEAD; ++d)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) tokens[d][q] = make_uint4(0u, 0u, 0u, 0u);      // stays so in lanes without a token
-    auto fetch_codes = [&](int i, uint4 (&f)[2]) {
+        for (int o = 0; o < NT; ++o)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) tokens[d][o][q] = make_uint4(0u, 0u, 0u, 0u);      // stays so in lanes without a token
+    auto fetch_codes = [&](int i, int slot) {
         if (i < whole) {
-            f[0] = ld_once_16(reinterpret_cast<const uint4 *>(qa));
-            f[1] = ld_once_16(reinterpret_cast<const uint4 *>(qb));
+            copy_async_16(ring + slot * LT_CODE_BYTES, qa);
+            copy_async_16(ring + slot * LT_CODE_BYTES + LT_CODE_BYTES / 2, qb);
         }
+        copy_async_commit();                                     // a group a piece, empty past the end
         qa += code_step;
         qb += code_step;
     };
-    auto fetch_tokens = [&](int i, uint4 (&f)[4]) {
-        if (i < whole && have) {
+    auto fetch_tokens = [&](int i, uint4 (&f)[NT][4]) {
 #pragma unroll
-            for (int q = 0; q < 4; ++q) f[q] = ld_u32x4(xt + 8 * q);
-        }
+        for (int o = 0; o < NT; ++o)
+            if (i < whole && have[o]) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) f[o][q] = ld_u32x4(x[o] + xt + 8 * q);
+            }
         xt += x_step;
     };
 #pragma unroll
-    for (int d = 0; d < LT_AHEAD; ++d) fetch_codes(d, codes[d]);
+    for (int d = 0; d < LT_AHEAD; ++d) fetch_codes(d, d);
     // the levels of 16 channels: 512 bytes
     if (tid < LT_CHANNELS * LIN_LEVELS / 2) {
         const int ch = tid / (LIN_LEVELS / 2), j = j0 + ch < p.d_out ? j0 + ch : j0;
@@ -265,7 +290,7 @@ __global__ void __launch_bounds__(LT_THREADS, 2) linear_token_kernel(const Linea
             *(reinterpret_cast<const uint32_t *>(p.table + static_cast<size_t>(j) * LIN_LEVELS) + tid % (LIN_LEVELS / 2));
     }
 #pragma unroll
-    for (int d = 0; d < LT_X_AHEAD; ++d) fetch_tokens(d, tokens[d]);
+    for (int d = 0; d < X_AHEAD; ++d) fetch_tokens(d, tokens[d]);
     __syncthreads();
     // Thread = pair of codes; eight threads next to each other store to eight different channels' words of their rows.
 #pragma unroll
@@ -277,71 +302,78 @@ __global__ void __launch_bounds__(LT_THREADS, 2) linear_token_kernel(const Linea
             st_shared_16(tables + h * LT_TABLE_BYTES + tid * 128 + ch * 16, make_uint4(v, v, v, v));
         }
     __syncthreads();
-    float c0[4] = {0.f, 0.f, 0.f, 0.f}, c1[4] = {0.f, 0.f, 0.f, 0.f};
-    const uint32_t mine_a = tables + lane * 4, mine_b = mine_a + LT_TABLE_BYTES;
-    auto word = [](uint32_t base, uint32_t w, int byte) {
-        const uint32_t row = (byte == 0 ? w << 7 : w >> (8 * byte - 7)) & 0x7F80u;
-        uint32_t v;
-        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(row | base));
-        return v;
+    float c0[NT][4] = {}, c1[NT][4] = {};
+    // (through the array itself: the tables' places are then part of the load's address)
+    auto word = [&](int table, uint32_t w, int byte) {
+        const uint32_t at = ((byte == 0 ? w << 7 : w >> (8 * byte - 7)) & 0x7F80u) | static_cast<uint32_t>(lane * 4);
+        return *reinterpret_cast<const uint32_t *>(smem_raw + table * LT_TABLE_BYTES + at);
     };
-    auto use = [&](const uint4 (&f)[2], const uint4 (&y)[4], int end) {
+    auto use = [&](const uint4 (&f)[2], const uint4 (&y)[NT][4], int end) {
         const uint32_t qa[4] = {f[0].x, f[0].y, f[0].z, f[0].w}, qb[4] = {f[1].x, f[1].y, f[1].z, f[1].w};
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             uint32_t wa[4], wb[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                wa[e] = word(mine_a, qa[q], e);
-                wb[e] = word(mine_b, qb[q], e);
+                wa[e] = word(0, qa[q], e);
+                wb[e] = word(1, qb[q], e);
             }
             if (8 * q >= end) {                                       // (never in a whole piece) no level meets padding
 #pragma unroll
                 for (int e = 0; e < 4; ++e) wa[e] = wb[e] = 0u;
             }
-            mma_m16n8k16<BF16>(c0, wa[0], wb[0], wa[1], wb[1], y[q].x, y[q].y);
-            mma_m16n8k16<BF16>(c1, wa[2], wb[2], wa[3], wb[3], y[q].z, y[q].w);
+#pragma unroll
+            for (int o = 0; o < NT; ++o) {
+                mma_m16n8k16<BF16>(c0[o], wa[0], wb[0], wa[1], wb[1], y[o][q].x, y[o][q].y);
+                mma_m16n8k16<BF16>(c1[o], wa[2], wb[2], wa[3], wb[3], y[o][q].z, y[o][q].w);
+            }
         }
     };
     for (int i = 0; i < whole; i += LT_AHEAD) {
 #pragma unroll
         for (int d = 0; d < LT_AHEAD; ++d) {
             if (i + d >= whole) break;
-            use(codes[d], tokens[d % LT_X_AHEAD], LT_K);
-            fetch_codes(i + d + LT_AHEAD, codes[d]);
-            fetch_tokens(i + d + LT_X_AHEAD, tokens[d % LT_X_AHEAD]);
+            copy_async_wait<LT_AHEAD - 1>();
+            const uint4 f[2] = {ld_shared_16(ring + d * LT_CODE_BYTES), ld_shared_16(ring + d * LT_CODE_BYTES + LT_CODE_BYTES / 2)};
+            use(f, tokens[d % X_AHEAD], LT_K);
+            fetch_codes(i + d + LT_AHEAD, d);                    // into what has been read and used
+            fetch_tokens(i + d + X_AHEAD, tokens[d % X_AHEAD]);
         }
     }
     if (ragged) {
         const int k = full * LT_K + 32 * t;
-        uint4 f[2] = {make_uint4(0u, 0u, 0u, 0u), make_uint4(0u, 0u, 0u, 0u)}, y[4];
+        uint4 f[2] = {make_uint4(0u, 0u, 0u, 0u), make_uint4(0u, 0u, 0u, 0u)}, y[NT][4];
         if (k < p.d_in) {
             f[0] = ld_once_16(reinterpret_cast<const uint4 *>(ca + (k >> 1)));
             f[1] = ld_once_16(reinterpret_cast<const uint4 *>(cb + (k >> 1)));
         }
 #pragma unroll
-        for (int q = 0; q < 4; ++q) y[q] = (have && k + 8 * q < p.d_in) ? ld_u32x4(x + k + 8 * q) : make_uint4(0u, 0u, 0u, 0u);
+        for (int o = 0; o < NT; ++o)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) y[o][q] = (have[o] && k + 8 * q < p.d_in) ? ld_u32x4(x[o] + k + 8 * q) : make_uint4(0u, 0u, 0u, 0u);
         use(f, y, p.d_in - k);
     }
     // c[0], c[1]: channel g, tokens 2 t, 2 t + 1; c[2], c[3]: channel g + 8
 #pragma unroll
-    for (int e = 0; e < 4; ++e) sums[warp][2 * t + (e & 1)][g + (e >= 2 ? 8 : 0)] = c0[e] + c1[e];
+    for (int o = 0; o < NT; ++o)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sums[warp][o * LT_TOKENS + 2 * t + (e & 1)][g + (e >= 2 ? 8 : 0)] = c0[o][e] + c1[o][e];
     __syncthreads();
     const int token = tid / LT_CHANNELS, ch = tid % LT_CHANNELS;
     float z = 0.0f;
-    if (tid < LT_TOKENS * LT_CHANNELS) {
+    if (tid < TOKENS * LT_CHANNELS) {
 #pragma unroll
         for (int w = 0; w < LT_WARPS; ++w) z += sums[w][token][ch];
         mine[tid] = z;
     }
     if (ranks > 1) {
         cluster_sync_all();
-        if (rank == 0 && tid < LT_TOKENS * LT_CHANNELS) {
+        if (rank == 0 && tid < TOKENS * LT_CHANNELS) {
             for (int r = 1; r < ranks; ++r) z += ld_cluster_f32(map_to_cta(smem_u32(&mine[tid]), r));
         }
     }
     const int j = j0 + ch;
-    if (rank == 0 && tid < LT_TOKENS * LT_CHANNELS && token < p.n && j < p.d_out) {
+    if (rank == 0 && tid < TOKENS * LT_CHANNELS && token < p.n && j < p.d_out) {
         if (p.bias) z += half_value(ld_u16(p.bias + j), BF16);
         if (p.Z) p.Z[token * p.ld_z + j] = static_cast<uint16_t>(half_bits(z, BF16));
         float y = activate(z, p.act);
