@@ -1622,15 +1622,27 @@ int32_t gq_linear(const void *X, int32_t dtype, int64_t n, int64_t d_in, int64_t
     return GQ_OK;
 }
 
-// Pieces of a channel tile's work in the gradient of the levels: at most this many, so that the scratch does not depend on the device.
-static int64_t level_grad_max_runs(int64_t n, int64_t d_in, int64_t d_out)
+// Work of the gradient of the levels: pieces of at most LG_CHUNK_KSTEPS k-steps, none of them empty.
+struct LevelGradPlan {
+    int64_t ch_tiles, f_tiles, chunks, chunk_ksteps;
+};
+static LevelGradPlan level_grad_plan(int64_t n, int64_t d_in, int64_t d_out)
 {
-    const int64_t ch_tiles = (d_out + gq::TILE_M - 1) / gq::TILE_M;
+    LevelGradPlan P;
+    P.ch_tiles = (d_out + gq::TILE_M - 1) / gq::TILE_M;
+    P.f_tiles = (d_in + gq::TILE_N - 1) / gq::TILE_N;
     const int64_t ksteps = (n + gq::TILE_K - 1) / gq::TILE_K;
-    const int64_t units = (d_in + gq::TILE_N - 1) / gq::TILE_N * ((ksteps + gq::LG_CHUNK_KSTEPS - 1) / gq::LG_CHUNK_KSTEPS);
-    int64_t runs = 160 / ch_tiles;
-    if (runs > units) runs = units;
-    return runs < 1 ? 1 : runs;
+    P.chunks = (ksteps + gq::LG_CHUNK_KSTEPS - 1) / gq::LG_CHUNK_KSTEPS;
+    P.chunk_ksteps = P.chunks ? (ksteps + P.chunks - 1) / P.chunks : 0;
+    if (P.chunks) P.chunks = (ksteps + P.chunk_ksteps - 1) / P.chunk_ksteps;
+    return P;
+}
+// Parts that a channel tile's sums can come in, with at most kLevelGradPairs pairs: the scratch does not depend on the device.
+constexpr int kLevelGradPairs = 80;
+static int64_t level_grad_max_parts(const LevelGradPlan &P)
+{
+    const int64_t per = P.f_tiles * P.chunks, parts = kLevelGradPairs / P.ch_tiles + 2;
+    return parts < per ? parts : (per > 0 ? per : 1);
 }
 
 struct LinearGradLayout {
@@ -1644,7 +1656,7 @@ static LinearGradLayout linear_grad_layout(int64_t n, int64_t d_in, int64_t d_ou
     if (L.rows_per_block < gq::LZ_MIN_ROWS) L.rows_per_block = gq::LZ_MIN_ROWS;
     L.blocks = (n + L.rows_per_block - 1) / L.rows_per_block;
     L.partial = 0;
-    L.sums = round_up(static_cast<size_t>(level_grad_max_runs(n, d_in, d_out)) * 2 * d_out * gq::LIN_LEVELS * 4, 1024);
+    L.sums = round_up(static_cast<size_t>(level_grad_max_parts(level_grad_plan(n, d_in, d_out))) * 2 * d_out * gq::LIN_LEVELS * 4, 1024);
     L.total = L.sums + round_up(static_cast<size_t>(L.blocks) * d_out * 4, 1024);
     return L;
 }
@@ -1725,7 +1737,11 @@ int32_t gq_linear_grad(const void *dY, int32_t dtype, int64_t n, int64_t d_out, 
         p.ld_out = ld_dx;
         if (int32_t rc = linear_pair(true, p, dtype, grad, ld_grad, m, di, st)) return rc;
     }
-    int parts = 0;
+    const LevelGradPlan P = level_grad_plan(n, d_in, d_out);
+    const int64_t per_tile = P.f_tiles * P.chunks, units = P.ch_tiles * per_tile;
+    if (units >= (1ll << 40)) return GQ_ERR_UNSUPPORTED_SHAPE;
+    int pairs = di->max_pairs < kLevelGradPairs ? di->max_pairs : kLevelGradPairs;
+    if (units < pairs) pairs = static_cast<int>(units);
     if (d_table) {
         gq::LevelGradParams p{};
         p.codes = codes;
@@ -1734,30 +1750,14 @@ int32_t gq_linear_grad(const void *dY, int32_t dtype, int64_t n, int64_t d_out, 
         p.d_in = static_cast<int>(d_in);
         p.d_out = static_cast<int>(d_out);
         p.bf16 = bf16;
-        p.ch_tiles = static_cast<int>((d_out + gq::TILE_M - 1) / gq::TILE_M);
-        p.f_tiles = static_cast<int>((d_in + gq::TILE_N - 1) / gq::TILE_N);
-        const int ksteps = static_cast<int>((n + gq::TILE_K - 1) / gq::TILE_K);
-        p.chunks = (ksteps + gq::LG_CHUNK_KSTEPS - 1) / gq::LG_CHUNK_KSTEPS;
-        p.chunk_ksteps = (ksteps + p.chunks - 1) / p.chunks;
-        p.chunks = (ksteps + p.chunk_ksteps - 1) / p.chunk_ksteps;       // no piece is empty
-        const int64_t units = static_cast<int64_t>(p.f_tiles) * p.chunks;
-        if (units >= (1ll << 30)) return GQ_ERR_UNSUPPORTED_SHAPE;
-        // Runs of a channel tile: as many as make the pair with the most units have the fewest.
-        int64_t most = level_grad_max_runs(n, d_in, d_out), least = INT64_MAX;
-        if (most > units) most = units;
-        for (int64_t r = 1; r <= most; ++r) {
-            const int64_t longest = (p.ch_tiles * r + di->max_pairs - 1) / di->max_pairs * ((units + r - 1) / r);
-            if (longest < least) {
-                least = longest;
-                p.runs = static_cast<int>(r);
-            }
-        }
-        const int64_t items = static_cast<int64_t>(p.ch_tiles) * p.runs;
-        p.pairs = items < di->max_pairs ? static_cast<int>(items) : di->max_pairs;
+        p.ch_tiles = static_cast<int>(P.ch_tiles);
+        p.f_tiles = static_cast<int>(P.f_tiles);
+        p.chunks = static_cast<int>(P.chunks);
+        p.chunk_ksteps = static_cast<int>(P.chunk_ksteps);
+        p.pairs = pairs;
         p.partial = reinterpret_cast<float *>(ws + L.partial);
         p.status = di->status_ptr;
         p.wait_budget_ns = wait_budget_ns();
-        parts = 2 * p.runs;
         CUtensorMap mapG, mapX;
         if (int32_t rc = make_map(&mapG, grad, d_out, n, 1, ld_grad, n * ld_grad, map_type(dtype))) return rc;
         if (int32_t rc = make_map(&mapX, X, d_in, n, 1, ld_x, n * ld_x, map_type(dtype))) return rc;
@@ -1769,9 +1769,10 @@ int32_t gq_linear_grad(const void *dY, int32_t dtype, int64_t n, int64_t d_out, 
     }
     if (sums) {
         LaunchScope scope(GQ_KERNEL_LINEAR_AUX, st);
-        const int64_t threads = d_out * (gq::LIN_LEVELS + 1);
-        launch(gq::linear_sum_kernel, dim3(static_cast<unsigned>((threads + 255) / 256)), 256, 0, st, reinterpret_cast<const float *>(ws + L.partial), parts,
-               static_cast<int>(d_out), m, d_table, reinterpret_cast<const float *>(ws + L.sums), static_cast<int>(L.blocks), d_bias);
+        const int64_t table_ctas = d_table ? (d_out * gq::LIN_LEVELS + 255) / 256 : 0, bias_ctas = d_bias ? (d_out + 31) / 32 : 0;
+        launch(gq::linear_sum_kernel, dim3(static_cast<unsigned>(table_ctas + bias_ctas)), 256, 0, st, reinterpret_cast<const float *>(ws + L.partial),
+               static_cast<int>(per_tile), static_cast<int>(P.ch_tiles), pairs, static_cast<int>(d_out), m, d_table,
+               reinterpret_cast<const float *>(ws + L.sums), static_cast<int>(L.blocks), d_bias, static_cast<int>(table_ctas));
     }
     GQ_CUDA(cudaGetLastError());
     return GQ_OK;

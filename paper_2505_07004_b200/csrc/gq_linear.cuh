@@ -105,12 +105,25 @@ __device__ __forceinline__ float activate(float z, int act)
     if (act == LIN_GELU) return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
     return z;
 }
+// 1 / (1 + exp(-z)) to two or three units in the last place: the exponent -z log2 e in two terms, a Newton step on the reciprocal.  Half the
+// instructions of the library's exponential and division, behind which the activation gradient of 2048 x 4096 took 20 us.
+__device__ __forceinline__ float sigmoid(float z)
+{
+    const float t = fminf(z * -SC_LOG2E, 126.0f);
+    const float rest = fmaf(z, -SC_LOG2E, -t) + z * -1.9259629911266175e-8f;      // log2 e = SC_LOG2E + 1.926e-8
+    float e = exp2_fast(t);
+    e = fmaf(e, t == 126.0f ? 0.0f : rest * SC_LN2, e);
+    const float d = 1.0f + e;
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(d));
+    return fmaf(r, fmaf(-d, r, 1.0f), r);
+}
 // The slope's fp32 value decides how dZ is rounded, and the fp32 gradients are those of the rounded dZ: no fast approximations.
 __device__ __forceinline__ float activation_slope(float z, int act)
 {
     if (act == LIN_RELU) return z > 0.0f ? 1.0f : 0.0f;
     if (act == LIN_SILU) {
-        const float sig = 1.0f / (1.0f + expf(-z));
+        const float sig = sigmoid(z);
         return sig * (1.0f + z * (1.0f - sig));
     }
     if (act == LIN_GELU) return 0.5f * (1.0f + erff(z * 0.70710678118654752f)) + z * expf(-0.5f * z * z) * 0.39894228040143268f;
@@ -913,12 +926,12 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_consta
 // ------------------------------------------------------------------------------------------------ backward pass
 constexpr int LZ_COLUMNS = 256;           // columns of a block: 32 lanes x 8
 constexpr int LZ_WARPS = 8;
-constexpr int LZ_MIN_ROWS = 64;           // rows of a block, more where there would be too many blocks
-constexpr int LZ_MAX_BLOCKS = 256;
+constexpr int LZ_MIN_ROWS = 16;           // rows of a block, more where there would be too many blocks
+constexpr int LZ_MAX_BLOCKS = 128;
 
 // dz = dy act'(z), rounded to the activations' type, and per block of rows the column sums of the rounded values (db is their sum over
 // the blocks, in the blocks' order).  Without an activation dZ is null: dy is dz, only the sums are formed.
-__global__ void __launch_bounds__(32 * LZ_WARPS) linear_dz_kernel(const uint16_t *dY, long long ld_dy, const uint16_t *Z, long long ld_z, int act, int bf16,
+__global__ void __launch_bounds__(32 * LZ_WARPS, 4) linear_dz_kernel(const uint16_t *dY, long long ld_dy, const uint16_t *Z, long long ld_z, int act, int bf16,
                                                                   int n, int d_out, int rows_per_block, uint16_t *dZ, long long ld_dz, float *col_sums)
 {
     __shared__ float part[LZ_WARPS][LZ_COLUMNS];
@@ -928,31 +941,34 @@ __global__ void __launch_bounds__(32 * LZ_WARPS) linear_dz_kernel(const uint16_t
     griddep_launch();
     griddep_wait();
     float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (col < d_out) {
-        for (int i = r0 + warp; i < r1; i += LZ_WARPS) {
-            const uint4 y = ld_u32x4(dY + i * ld_dy + col);
-            const uint32_t *yw = reinterpret_cast<const uint32_t *>(&y);
+    // a warp's rows two at a time, all loads ahead of the first use
+    for (int i0 = r0 + warp; col < d_out && i0 < r1; i0 += 2 * LZ_WARPS) {
+        uint4 y[2], z[2];
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            const int i = i0 + q * LZ_WARPS;
+            y[q] = i < r1 ? ld_u32x4(dY + i * ld_dy + col) : make_uint4(0u, 0u, 0u, 0u);
+            if (dZ) z[q] = i < r1 ? ld_u32x4(Z + i * ld_z + col) : make_uint4(0u, 0u, 0u, 0u);
+        }
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            const int i = i0 + q * LZ_WARPS;
+            if (i >= r1) break;
+            uint32_t *yw = reinterpret_cast<uint32_t *>(&y[q]);
             if (dZ) {
-                const uint4 z = ld_u32x4(Z + i * ld_z + col);
-                const uint32_t *zw = reinterpret_cast<const uint32_t *>(&z);
-                uint4 out;
-                uint32_t *ow = reinterpret_cast<uint32_t *>(&out);
+                const uint32_t *zw = reinterpret_cast<const uint32_t *>(&z[q]);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const float2 a = half2_value(yw[e], bf16 != 0), b = half2_value(zw[e], bf16 != 0);
-                    ow[e] = half2_bits(a.x * activation_slope(b.x, act), a.y * activation_slope(b.y, act), bf16 != 0);
-                    const float2 kept = half2_value(ow[e], bf16 != 0);
-                    sum[2 * e] += kept.x;
-                    sum[2 * e + 1] += kept.y;
+                    yw[e] = half2_bits(a.x * activation_slope(b.x, act), a.y * activation_slope(b.y, act), bf16 != 0);
                 }
-                *reinterpret_cast<uint4 *>(dZ + i * ld_dz + col) = out;
-            } else {
+                *reinterpret_cast<uint4 *>(dZ + i * ld_dz + col) = y[q];
+            }
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float2 a = half2_value(yw[e], bf16 != 0);
-                    sum[2 * e] += a.x;
-                    sum[2 * e + 1] += a.y;
-                }
+            for (int e = 0; e < 4; ++e) {
+                const float2 kept = half2_value(yw[e], bf16 != 0);
+                sum[2 * e] += kept.x;
+                sum[2 * e + 1] += kept.y;
             }
         }
     }
@@ -976,50 +992,57 @@ struct LevelGradParams {
     int bf16;
     int ch_tiles, f_tiles, chunks;       // tiles of 256 channels and 256 features, pieces of the tokens
     int chunk_ksteps;                    // k-steps (of 64 tokens) of a piece
-    int runs;                            // pieces of a channel tile's f_tiles * chunks units, a partial sum each
-    int pairs;
-    float *partial;                      // [runs][2][d_out][16]
+    int pairs;                           // at most as many as there are units
+    float *partial;                      // [part of a channel tile][2][d_out][16]
     uint32_t *status;
     unsigned long long wait_budget_ns;
 };
 
+// Units (channel tile, feature tile, token piece), channel tiles outermost, are cut into equal runs, one a pair; a run ends up in two channel
+// tiles where it crosses from one to the next.  The parts of a channel tile are numbered by the pairs that have them.
+__host__ __device__ inline int level_grad_pair_of(long long unit, long long units, int pairs)
+{
+    return static_cast<int>(((unit + 1) * pairs - 1) / units);       // the last pair whose run starts at or before the unit
+}
+__host__ __device__ inline int level_grad_parts(int tile, int per_tile, int ch_tiles, int pairs)
+{
+    const long long units = static_cast<long long>(ch_tiles) * per_tile, first = static_cast<long long>(tile) * per_tile;
+    return level_grad_pair_of(first + per_tile - 1, units, pairs) - level_grad_pair_of(first, units, pairs) + 1;
+}
+
 struct LevelGradUnit {
-    int tile, run, f0, t0, t1;           // channel tile, run, first feature, k-steps [t0, t1)
-    bool last;                           // of its run
+    int tile, part, f0, t0, t1;          // channel tile, part of it, first feature, k-steps [t0, t1)
+    bool last;                           // of its part
 };
-// The units of a pair: runs pair, pair + pairs, ... of ch_tiles * runs, and within a run its share of (feature tile, token piece).
 struct LevelGradCursor {
     const LevelGradParams &p;
-    int item, unit, end;
-    __device__ LevelGradCursor(const LevelGradParams &pp, int pair) : p(pp), item(pair), unit(0), end(0) { open(); }
-    __device__ void open()
+    int pair;
+    long long unit, end, units;
+    __device__ LevelGradCursor(const LevelGradParams &pp, int pr) : p(pp), pair(pr)
     {
-        const int total = p.f_tiles * p.chunks, run = item % p.runs;
-        unit = static_cast<int>(static_cast<long long>(total) * run / p.runs);
-        end = static_cast<int>(static_cast<long long>(total) * (run + 1) / p.runs);
+        units = static_cast<long long>(p.ch_tiles) * p.f_tiles * p.chunks;
+        unit = units * pair / p.pairs;
+        end = units * (pair + 1) / p.pairs;
     }
     __device__ bool next(LevelGradUnit &u)
     {
-        if (unit == end) {
-            item += p.pairs;
-            open();
-        }
-        if (item >= p.ch_tiles * p.runs) return false;
-        u.tile = item / p.runs;
-        u.run = item % p.runs;
-        const int f = unit / p.chunks, c = unit - f * p.chunks;
-        const int ksteps = (p.n + TILE_K - 1) / TILE_K;
+        if (unit >= end) return false;
+        const int per = p.f_tiles * p.chunks;
+        u.tile = static_cast<int>(unit / per);
+        const int rest = static_cast<int>(unit - static_cast<long long>(u.tile) * per), f = rest / p.chunks, c = rest - f * p.chunks;
+        u.part = pair - level_grad_pair_of(static_cast<long long>(u.tile) * per, units, p.pairs);
         u.f0 = f * TILE_N;
         u.t0 = c * p.chunk_ksteps;
-        u.t1 = min(u.t0 + p.chunk_ksteps, ksteps);
-        u.last = ++unit == end;
+        u.t1 = min(u.t0 + p.chunk_ksteps, (p.n + TILE_K - 1) / TILE_K);
+        ++unit;
+        u.last = unit == end || rest == per - 1;
         return true;
     }
 };
 
 // Gradient of the levels: G[j][c] = sum_i dz_ij x_ic on the tensor cores (both operands by TMA, tokens as rows), never in memory: a lane
 // of the epilogue is a channel and adds its entries to the sum of the level their code names, in shared memory.  A pair keeps these
-// sums over a run of tiles and writes 16 numbers a channel at its end; the runs are added up in their order by linear_sum_kernel.
+// sums over its run of units and writes 16 numbers a channel at its end; the parts are added up in their order by linear_sum_kernel.
 // The tokens are taken in pieces of at most 1024: the tensor cores' accumulation truncates, so that long runs drift.
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LG_THREADS, 1)
 linear_level_grad_kernel(const __grid_constant__ CUtensorMap mapG, const __grid_constant__ CUtensorMap mapX, const LevelGradParams p)
@@ -1033,7 +1056,7 @@ linear_level_grad_kernel(const __grid_constant__ CUtensorMap mapG, const __grid_
     __shared__ uint32_t tmem_base_smem;
     __shared__ volatile uint32_t abort_flag;
 
-    const int warp = threadIdx.x >> 5;
+    const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0);
     const int lane = threadIdx.x & 31;
     const uint32_t rank = cluster_ctarank();
     const int pair = static_cast<int>(blockIdx.x >> 1);
@@ -1097,8 +1120,9 @@ linear_level_grad_kernel(const __grid_constant__ CUtensorMap mapG, const __grid_
             if (++s == LG_STAGES) { s = 0; ph ^= 1u; }
         }
         if (!ok) spin_ns(1000000ull);
-    } else if (warp == 3 && lane == 0 && rank == 0) {
-        // ------------------------------------------------------------------ MMA issuer (first CTA)
+    } else if (warp == 3 && rank == 0) {
+        // ------------------------------------------------------------------ MMA issuer (first CTA; see linear_pair_kernel)
+        const bool elected = elect_one();
         const uint32_t idesc = umma_idesc_16(TILE_M, TILE_N, p.bf16 != 0, true, true);
         int s = 0;
         uint32_t ph = 0;
@@ -1108,29 +1132,29 @@ linear_level_grad_kernel(const __grid_constant__ CUtensorMap mapG, const __grid_
         LevelGradCursor cur(p, pair);
         LevelGradUnit u;
         while (ok && cur.next(u)) {
-            if (!bounded_wait_hot(smem_u32(&bar_acc_empty[buf]), ((acc_ph >> buf) & 1u) ^ 1u, wc, 2u, u.tile)) { ok = false; break; }
+            if (!warp_wait_hot(smem_u32(&bar_acc_empty[buf]), ((acc_ph >> buf) & 1u) ^ 1u, wc, 2u, u.tile)) { ok = false; break; }
             tc_fence_after_sync();
             const uint32_t d_tmem = tmem_base + static_cast<uint32_t>(buf * TILE_N);
             for (int kb = u.t0; kb < u.t1; ++kb) {
-                if (!bounded_wait_hot(smem_u32(&bar_full[s]), ph, wc, 3u, u.tile)) { ok = false; break; }
+                if (!warp_wait_hot(smem_u32(&bar_full[s]), ph, wc, 3u, u.tile)) { ok = false; break; }
                 tc_fence_after_sync();
                 const uint32_t sa = ring + s * LG_STAGE_BYTES;
-                const uint32_t sb = sa + LP_SLOT_BYTES;
+                const uint64_t adesc = umma_smem_desc_mn_sw128(sa, BOX_BYTES, 1024), bdesc = umma_smem_desc_mn_sw128(sa + LP_SLOT_BYTES, BOX_BYTES, 1024);
+                constexpr uint64_t step = (16 * 128) >> 4;
+                if (elected) {
+                    umma_bf16(d_tmem, adesc, bdesc, idesc, kb != u.t0 ? 1u : 0u);
 #pragma unroll
-                for (int k16 = 0; k16 < TILE_K / 16; ++k16) {
-                    const uint64_t adesc = umma_smem_desc_mn_sw128(sa + k16 * 16 * 128, BOX_BYTES, 1024);
-                    const uint64_t bdesc = umma_smem_desc_mn_sw128(sb + k16 * 16 * 128, BOX_BYTES, 1024);
-                    umma_bf16(d_tmem, adesc, bdesc, idesc, (kb != u.t0 || k16 != 0) ? 1u : 0u);
+                    for (int k16 = 1; k16 < TILE_K / 16; ++k16) umma_bf16(d_tmem, adesc + k16 * step, bdesc + k16 * step, idesc, 1u);
+                    umma_commit_pair(smem_u32(&bar_empty[s]));
                 }
-                umma_commit_pair(smem_u32(&bar_empty[s]));
                 if (++s == LG_STAGES) { s = 0; ph ^= 1u; }
             }
             if (!ok) break;
-            umma_commit_pair(smem_u32(&bar_acc_full[buf]));
+            if (elected) umma_commit_pair(smem_u32(&bar_acc_full[buf]));
             acc_ph ^= 1u << buf;
             buf ^= 1;
         }
-        if (!ok) {
+        if (!ok && elected) {
             // Make sure no MMA is still writing TMEM when it is released.
             umma_commit_local(smem_u32(&bar_drain));
             const uint64_t t0 = global_timer_ns();
@@ -1187,7 +1211,7 @@ linear_level_grad_kernel(const __grid_constant__ CUtensorMap mapG, const __grid_
                     sums[l * 32] = 0.0f;
                 }
                 if (have) {
-                    float4 *out = reinterpret_cast<float4 *>(p.partial + ((static_cast<size_t>(u.run) * 2 + half) * p.d_out + j) * LIN_LEVELS);
+                    float4 *out = reinterpret_cast<float4 *>(p.partial + ((static_cast<size_t>(u.part) * 2 + half) * p.d_out + j) * LIN_LEVELS);
 #pragma unroll
                     for (int l = 0; l < LIN_LEVELS / 4; ++l) out[l] = make_float4(v[4 * l], v[4 * l + 1], v[4 * l + 2], v[4 * l + 3]);
                 }
@@ -1205,24 +1229,42 @@ linear_level_grad_kernel(const __grid_constant__ CUtensorMap mapG, const __grid_
     }
 }
 
-// Sums of the partial results in their order, in 64 bits: d_table [d_out][m] from `parts` parts, d_bias [d_out] from `blocks` rows.
-__global__ void __launch_bounds__(256) linear_sum_kernel(const float *partial, int parts, int d_out, int m, float *d_table, const float *col_sums,
-                                                         int blocks, float *d_bias)
+// Sums of the partial results in their order, in 64 bits: d_table [d_out][m] from the parts of each channel tile (a thread a cell), d_bias
+// [d_out] from `blocks` rows of column sums (32 channels a CTA, every eighth row a thread).
+__global__ void __launch_bounds__(256) linear_sum_kernel(const float *partial, int per_tile, int ch_tiles, int pairs, int d_out, int m, float *d_table,
+                                                         const float *col_sums, int blocks, float *d_bias, int table_ctas)
 {
+    __shared__ double part[8][32];
     griddep_launch();
     griddep_wait();
-    const long long i = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x, cells = static_cast<long long>(d_out) * LIN_LEVELS;
-    if (i < cells) {
-        if (!d_table) return;
-        const int j = static_cast<int>(i / LIN_LEVELS), l = static_cast<int>(i % LIN_LEVELS);
-        if (l >= m) return;
+    auto sum = [](const float *src, long long stride, int count) {
         double total = 0.0;
-        for (int r = 0; r < parts; ++r) total += static_cast<double>(partial[static_cast<size_t>(r) * cells + i]);
-        d_table[static_cast<size_t>(j) * m + l] = static_cast<float>(total);
-    } else if (i - cells < d_out && d_bias) {
+        for (int r0 = 0; r0 < count; r0 += 8) {
+            float v[8];
+#pragma unroll
+            for (int q = 0; q < 8; ++q) v[q] = r0 + q < count ? src[(r0 + q) * stride] : 0.0f;
+#pragma unroll
+            for (int q = 0; q < 8; ++q) total += static_cast<double>(v[q]);
+        }
+        return total;
+    };
+    if (static_cast<int>(blockIdx.x) < table_ctas) {
+        const long long i = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x, cells = static_cast<long long>(d_out) * LIN_LEVELS;
+        const int level = static_cast<int>(i % LIN_LEVELS);
+        if (i >= cells || level >= m) return;
+        const int count = 2 * level_grad_parts(static_cast<int>(i / (LIN_LEVELS * TILE_M)), per_tile, ch_tiles, pairs);
+        d_table[i / LIN_LEVELS * m + level] = static_cast<float>(sum(partial + i, cells, count));
+        return;
+    }
+    const int j = (static_cast<int>(blockIdx.x) - table_ctas) * 32 + static_cast<int>(threadIdx.x & 31), share = static_cast<int>(threadIdx.x >> 5);
+    part[share][threadIdx.x & 31] =
+        j < d_out && share < blocks ? sum(col_sums + static_cast<size_t>(share) * d_out + j, 8ll * d_out, (blocks - share + 7) / 8) : 0.0;
+    __syncthreads();
+    if (share == 0 && j < d_out) {
         double total = 0.0;
-        for (int b = 0; b < blocks; ++b) total += static_cast<double>(col_sums[static_cast<size_t>(b) * d_out + (i - cells)]);
-        d_bias[i - cells] = static_cast<float>(total);
+#pragma unroll
+        for (int w = 0; w < 8; ++w) total += part[w][threadIdx.x];
+        d_bias[j] = static_cast<float>(total);
     }
 }
 

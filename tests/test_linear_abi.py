@@ -31,9 +31,9 @@ def test_sizes(L):
     assert L.gq_linear_codes_bytes(72, 24) == 24 * 48                   # rows padded to whole 16 bytes
     assert L.gq_linear_codes_bytes(68, 24) == 0 and L.gq_linear_codes_bytes(64, 20) == 0 and L.gq_linear_codes_bytes(0, 8) == 0
     assert L.gq_linear_codes_bytes((1 << 20) + 8, 8) == 0
-    # one run of partial sums for both halves of a feature tile (256 channels are one tile), one row of column sums
-    assert L.gq_linear_grad_workspace_bytes(64, 256, 256) == 2 * 256 * 64 + 1024
-    assert L.gq_linear_grad_workspace_bytes(65, 256, 264) == 2 * 264 * 64 + (2 * 264 * 4 + 1023) // 1024 * 1024
+    # one part of sums for both halves of a feature tile (256 channels are one tile), one row of column sums for 16 tokens
+    assert L.gq_linear_grad_workspace_bytes(16, 256, 256) == 2 * 256 * 64 + 1024
+    assert L.gq_linear_grad_workspace_bytes(17, 256, 264) == 2 * 264 * 64 + (2 * 264 * 4 + 1023) // 1024 * 1024
     assert L.gq_linear_grad_workspace_bytes(-1, 256, 256) == 0 and L.gq_linear_grad_workspace_bytes(1, 255, 256) == 0
 
 
