@@ -11,6 +11,10 @@ two passes over the same calibration batches in the same order:
         for batch in batches: model(batch)
     H = cap.finalize()                   # {name: [g, d_in, d_in] fp32}, complete symmetric matrices
 
+With the end loss of next-token prediction both passes are one call, cap.calibrate(model, [(inputs, targets), ...]), whose backward pass
+starts from loss.end_loss.  Layers may be quantised already (quantized.QuantizedLinear): their saliencies are those of the
+pre-activation's gradient.
+
 No arithmetic of the method happens here.  The backward hook hands the gradient over as autograd produced it
 (``[batch, seq, d_out]`` in bf16, fp16 or fp32, any batch / sequence strides) to gq_saliency_strided, so no cast
 and no contiguous copy of it is ever made; other layouts are flattened and cast to bf16 for gq_saliency.  The
@@ -24,6 +28,8 @@ from typing import Dict
 import torch
 
 from . import api
+from .loss import end_loss
+from .quantized import QuantizedLinear
 
 
 class GuidedHessianCapture:
@@ -45,14 +51,16 @@ class GuidedHessianCapture:
         """Registers backward hooks; every backward call appends one saliency block per layer."""
         handles = []
         for name, mod in self.layers.items():
-            def hook(_mod, _grad_in, grad_out, name=name):
-                grad = grad_out[0].detach()
+            def take(grad, name=name):
                 if (grad.dim() == 3 and grad.dtype in (torch.bfloat16, torch.float16, torch.float32)
                         and (grad.shape[2] == 1 or grad.stride(2) == 1)):
                     self.s[name].append(api.gq_saliency_strided(grad, self.g, self.grad_scale))
                 else:
                     self.s[name].append(api.gq_saliency(self._tokens(grad), self.g, self.grad_scale))
-            handles.append(mod.register_full_backward_hook(hook))
+            if isinstance(mod, QuantizedLinear):
+                handles.append(mod.register_pre_activation_hook(take))
+            else:
+                handles.append(mod.register_full_backward_hook(lambda _mod, _grad_in, grad_out, take=take: take(grad_out[0].detach())))
         try:
             yield self
         finally:
@@ -87,6 +95,18 @@ class GuidedHessianCapture:
         finally:
             for h in handles:
                 h.remove()
+
+    def calibrate(self, model, batches) -> Dict[str, torch.Tensor]:
+        """Both passes over ``(inputs, targets)`` batches with the end loss of ``model(inputs)`` (logits ``[..., vocab]``), then finalize.
+        Gradients that the backward passes leave in the parameters are dropped."""
+        with self.saliency_pass():
+            for inputs, targets in batches:
+                end_loss(model(inputs), targets).backward()
+                model.zero_grad(set_to_none=True)
+        with self.hessian_pass(), torch.no_grad():
+            for inputs, _ in batches:
+                model(inputs)
+        return self.finalize()
 
     def finalize(self) -> Dict[str, torch.Tensor]:
         for name, H in self.H.items():
