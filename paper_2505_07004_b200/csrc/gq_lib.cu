@@ -115,7 +115,7 @@ struct DeviceInfo {
     bool ready = false;
     int sm_count = 0;
     int max_pairs = 0;          // CTA pairs (clusters of two) of a tensor-core kernel that can be resident at once
-    int split_clusters[2] = {0, 0};      // clusters of two and of four pairs of linear_pair_kernel that can be
+    int split_clusters[3] = {0, 0, 0};   // clusters of two, four and eight pairs of linear_pair_kernel that can be
     uint32_t *status_ptr = nullptr;
 };
 DeviceInfo g_dev[kMaxDevices];
@@ -195,12 +195,16 @@ int32_t device_info(DeviceInfo **out)
         GQ_CUDA(cudaFuncSetAttribute(gq::cd_block_kernel<16, 16>, cudaFuncAttributeMaxDynamicSharedMemorySize, gq::cd_smem_bytes(16)));
         GQ_CUDA(cudaFuncSetAttribute(gq::linear_pair_kernel<false, false, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, gq::LP_SMEM_BYTES));
         GQ_CUDA(cudaFuncSetAttribute(gq::linear_pair_kernel<false, false, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, gq::LP_SMEM_BYTES));
+        GQ_CUDA(cudaFuncSetAttribute(gq::linear_pair_kernel<false, false, true>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
         GQ_CUDA(cudaFuncSetAttribute(gq::linear_pair_kernel<false, true, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, gq::LP_SMEM_BYTES));
         GQ_CUDA(cudaFuncSetAttribute(gq::linear_pair_kernel<false, true, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, gq::LP_SMEM_BYTES));
+        GQ_CUDA(cudaFuncSetAttribute(gq::linear_pair_kernel<false, true, true>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
         GQ_CUDA(cudaFuncSetAttribute(gq::linear_pair_kernel<true, false, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, gq::LP_SMEM_BYTES));
         GQ_CUDA(cudaFuncSetAttribute(gq::linear_pair_kernel<true, false, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, gq::LP_SMEM_BYTES));
+        GQ_CUDA(cudaFuncSetAttribute(gq::linear_pair_kernel<true, false, true>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
         GQ_CUDA(cudaFuncSetAttribute(gq::linear_pair_kernel<true, true, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, gq::LP_SMEM_BYTES));
         GQ_CUDA(cudaFuncSetAttribute(gq::linear_pair_kernel<true, true, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, gq::LP_SMEM_BYTES));
+        GQ_CUDA(cudaFuncSetAttribute(gq::linear_pair_kernel<true, true, true>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
         GQ_CUDA(cudaFuncSetAttribute(gq::linear_token_kernel<true, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, gq::LT_SMEM_BYTES));
         GQ_CUDA(cudaFuncSetAttribute(gq::linear_token_kernel<true, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, gq::LT_SMEM_BYTES));
         GQ_CUDA(cudaFuncSetAttribute(gq::linear_token_kernel<false, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, gq::LT_SMEM_BYTES));
@@ -230,7 +234,7 @@ int32_t device_info(DeviceInfo **out)
             if (clusters < 1) clusters = 1;
             di.max_pairs = clusters;
         }
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < 3; ++i) {
             cudaLaunchConfig_t cfg = {};
             cudaLaunchAttribute attr;
             attr.id = cudaLaunchAttributeClusterDimension;
@@ -1527,13 +1531,13 @@ static int32_t linear_pair(bool back, gq::LinearParams p, int32_t dtype, const v
     p.doubles = static_cast<int>(2 * rest <= di->max_pairs && p.n > gq::TILE_N ? tiles - rest : tiles);
     p.units = p.doubles + 2 * (static_cast<int>(tiles) - p.doubles);
     p.pairs = p.units < di->max_pairs ? p.units : di->max_pairs;
-    // Few tiles of 256 x 256: the contraction is split over the pairs of a cluster, up to four of them with four k-steps each at least,
+    // Few tiles of 256 x 256: the contraction is split over the pairs of a cluster, up to eight of them with four k-steps each at least,
     // while all clusters are resident at once (4096 x 4096, 256 tokens: 16 clusters of eight CTAs, two of which wait for the others,
     // take 45 us, of four CTAs 37).
     const int64_t singles = row_tiles * ((p.n + gq::TILE_N - 1) / gq::TILE_N);
     const int ksteps = (kdim + gq::TILE_K - 1) / gq::TILE_K;
     p.ranks = 1;
-    while (p.ranks < gq::LP_MAX_SPLIT && singles <= di->split_clusters[p.ranks - 1] && ksteps >= 8 * p.ranks) p.ranks *= 2;
+    for (int i = 0; p.ranks < gq::LP_MAX_SPLIT && singles <= di->split_clusters[i] && ksteps >= 8 * p.ranks; ++i) p.ranks *= 2;
     const bool split = p.ranks > 1;
     if (split) p.pairs = static_cast<int>(singles) * p.ranks;
     p.ntile = p.n < gq::TILE_N ? (p.n + 31) / 32 * 32 : gq::TILE_N;

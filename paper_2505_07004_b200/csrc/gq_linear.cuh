@@ -268,16 +268,16 @@ __global__ void __launch_bounds__(LT_THREADS, 2) linear_token_kernel(const Linea
         x[o] = p.X + static_cast<long long>(have[o] ? g + o * LT_TOKENS : 0) * p.ld_x;
     }
     const int pieces = (p.d_in + LT_K - 1) / LT_K, stride = ranks * LT_WARPS;
-    // A warp's pieces are rank * LT_WARPS + warp, + stride, ...; the `whole` first of them lie inside the row, one ragged piece may follow.
+    // A warp takes pairs of neighbouring pieces (128 bytes of a channel's codes): pairs base, base + stride, ...  The `whole` first of its pieces
+    // lie inside the row, one ragged piece may follow.
     // Codes come from device memory, by asynchronous copies LT_AHEAD pieces ahead: each lane copies and reads its own 16 bytes, so nothing but
     // its own wait is needed; in registers the loads of four pieces shared the few scoreboards there are, and waits for one waited
     // for the others.  Activations come from L2 or L1, one or two pieces ahead, in registers.
-    const int first = rank * LT_WARPS + warp, full = p.d_in / LT_K;
-    const int whole = first < full ? (full - first + stride - 1) / stride : 0;
-    const bool ragged = full < pieces && full % stride == first;
-    const uint8_t *qa = ca + (first * LT_K + 32 * t) / 2, *qb = cb + (first * LT_K + 32 * t) / 2;
-    size_t xt = static_cast<size_t>(first) * LT_K + 32 * t;
-    const size_t code_step = static_cast<size_t>(stride) * LT_K / 2, x_step = static_cast<size_t>(stride) * LT_K;
+    const int base = rank * LT_WARPS + warp, full = p.d_in / LT_K, last_pair = full / 2;
+    const int whole = (base < last_pair ? 2 * ((last_pair - base + stride - 1) / stride) : 0) + ((full & 1) != 0 && last_pair % stride == base ? 1 : 0);
+    const bool ragged = full < pieces && last_pair % stride == base;
+    // contraction index of the i-th piece, for this lane
+    auto index_of = [&](int i) { return ((base + (i >> 1) * stride) * 2 + (i & 1)) * LT_K + 32 * t; };
     uint4 tokens[X_AHEAD][NT][4];
 #pragma unroll
     for (int d = 0; d < X_AHEAD; ++d)
@@ -287,21 +287,19 @@ __global__ void __launch_bounds__(LT_THREADS, 2) linear_token_kernel(const Linea
             for (int q = 0; q < 4; ++q) tokens[d][o][q] = make_uint4(0u, 0u, 0u, 0u);      // stays so in lanes without a token
     auto fetch_codes = [&](int i, int slot) {
         if (i < whole) {
-            copy_async_16(ring + slot * LT_CODE_BYTES, qa);
-            copy_async_16(ring + slot * LT_CODE_BYTES + LT_CODE_BYTES / 2, qb);
+            const int at = index_of(i) >> 1;
+            copy_async_16(ring + slot * LT_CODE_BYTES, ca + at);
+            copy_async_16(ring + slot * LT_CODE_BYTES + LT_CODE_BYTES / 2, cb + at);
         }
         copy_async_commit();                                     // a group a piece, empty past the end
-        qa += code_step;
-        qb += code_step;
     };
     auto fetch_tokens = [&](int i, uint4 (&f)[NT][4]) {
 #pragma unroll
         for (int o = 0; o < NT; ++o)
             if (i < whole && have[o]) {
 #pragma unroll
-                for (int q = 0; q < 4; ++q) f[o][q] = ld_u32x4(x[o] + xt + 8 * q);
+                for (int q = 0; q < 4; ++q) f[o][q] = ld_u32x4(x[o] + index_of(i) + 8 * q);
             }
-        xt += x_step;
     };
 #pragma unroll
     for (int d = 0; d < LT_AHEAD; ++d) fetch_codes(d, d);
@@ -315,14 +313,16 @@ __global__ void __launch_bounds__(LT_THREADS, 2) linear_token_kernel(const Linea
     for (int d = 0; d < X_AHEAD; ++d) fetch_tokens(d, tokens[d]);
     __syncthreads();
     // Thread = pair of codes; eight threads next to each other store to eight different channels' words of their rows.
+    if (tid < 256) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int ch = (i + tid) & 7;
-            const uint32_t v = static_cast<uint32_t>(levels[8 * h + ch][tid & 15]) | (static_cast<uint32_t>(levels[8 * h + ch][tid >> 4]) << 16);
-            st_shared_16(tables + h * LT_TABLE_BYTES + tid * 128 + ch * 16, make_uint4(v, v, v, v));
-        }
+            for (int i = 0; i < 8; ++i) {
+                const int ch = (i + tid) & 7;
+                const uint32_t v = static_cast<uint32_t>(levels[8 * h + ch][tid & 15]) | (static_cast<uint32_t>(levels[8 * h + ch][tid >> 4]) << 16);
+                st_shared_16(tables + h * LT_TABLE_BYTES + tid * 128 + ch * 16, make_uint4(v, v, v, v));
+            }
+    }
     __syncthreads();
     float c0[NT][4] = {}, c1[NT][4] = {};
     // (through the array itself: the tables' places are then part of the load's address)
@@ -419,10 +419,11 @@ constexpr int LP_LOOK_WARPS = 4 * LP_LOOK_GROUPS;
 constexpr int LP_EPI_WARPS = 8;
 constexpr int LP_THREADS = 32 * (4 + LP_LOOK_WARPS + LP_EPI_WARPS);
 constexpr int LP_SMEM_BYTES = LP_STAGES * LP_STAGE_BYTES + LP_CODE_SLOTS * LP_CODE_BYTES + 1024;
-constexpr int LP_MAX_SPLIT = 4;                                           // pairs of a cluster (eight CTAs)
-constexpr int LG_STAGES = 6;                                              // gradient of the levels
+constexpr int LP_MAX_SPLIT = 8;                                           // pairs of a cluster (sixteen CTAs)
+constexpr int LG_STAGES = 4;                                              // gradient of the levels
+constexpr int LG_SETS = 4;                                                // sums of a channel that are added to in turn
 constexpr int LG_STAGE_BYTES = 2 * LP_SLOT_BYTES;                         // [dZ | tokens]
-constexpr int LG_SMEM_BYTES = LG_STAGES * LG_STAGE_BYTES + LP_EPI_WARPS * LIN_LEVELS * 32 * 4 + 1024;
+constexpr int LG_SMEM_BYTES = LG_STAGES * LG_STAGE_BYTES + LP_EPI_WARPS * LG_SETS * LIN_LEVELS * 32 * 4 + 1024;
 constexpr int LG_THREADS = 32 * (4 + LP_EPI_WARPS);
 constexpr int LG_CHUNK_KSTEPS = 16;                                       // 1024 tokens
 constexpr int LP_ROW_BLOCK = 16;                                          // row tiles that are worked on beside each other
@@ -1172,9 +1173,10 @@ linear_level_grad_kernel(const __grid_constant__ CUtensorMap mapG, const __grid_
         const int ew = warp - 4;                        // 0..7; four consecutive warps cover the four lane quarters
         const int q = warp & 3;                         // TMEM lane quarter this warp may access
         const int half = ew >> 2;                       // which 128 of the 256 features
-        float *sums = reinterpret_cast<float *>(smem_raw + (ring - smem_u32(smem_raw)) + LG_STAGES * LG_STAGE_BYTES) + ew * LIN_LEVELS * 32 + lane;
-#pragma unroll
-        for (int l = 0; l < LIN_LEVELS; ++l) sums[l * 32] = 0.0f;
+        float *sums = reinterpret_cast<float *>(smem_raw + (ring - smem_u32(smem_raw)) + LG_STAGES * LG_STAGE_BYTES) +
+                      ew * LG_SETS * LIN_LEVELS * 32 + lane;
+#pragma unroll 16
+        for (int l = 0; l < LG_SETS * LIN_LEVELS; ++l) sums[l * 32] = 0.0f;
         uint32_t full_ph = 0u;                          // bit b: phase of accumulator b
         int buf = 0;
         bool ok = true;
@@ -1206,16 +1208,31 @@ linear_level_grad_kernel(const __grid_constant__ CUtensorMap mapG, const __grid_
                     if (lane == 0) mbar_arrive_cluster(map_to_cta(smem_u32(&bar_acc_empty[buf]), 0));
                 }
                 const uint32_t w[4] = {codes[x].x, codes[x].y, codes[x].z, codes[x].w};
-                // features behind d_in: their column of G is zero and so is their code
+                // Features behind d_in: their column of G is zero and so is their code.  Four entries at a time, each into sums of its own, so that
+                // their loads, additions and stores overlap: one after the other 128 of them took 4500 clocks.
 #pragma unroll
-                for (int e = 0; e < 32; ++e) sums[((w[e >> 3] >> (4 * (e & 7))) & 15u) * 32] += __uint_as_float(acc[e]);
+                for (int e = 0; e < 32; e += LG_SETS) {
+                    float v[LG_SETS];
+                    int at[LG_SETS];
+#pragma unroll
+                    for (int k = 0; k < LG_SETS; ++k) {
+                        at[k] = (k * LIN_LEVELS + static_cast<int>((w[(e + k) >> 3] >> (4 * ((e + k) & 7))) & 15u)) * 32;
+                        v[k] = sums[at[k]];
+                    }
+#pragma unroll
+                    for (int k = 0; k < LG_SETS; ++k) sums[at[k]] = v[k] + __uint_as_float(acc[e + k]);
+                }
             }
             if (u.last) {
                 float v[LIN_LEVELS];
 #pragma unroll
                 for (int l = 0; l < LIN_LEVELS; ++l) {
-                    v[l] = sums[l * 32];
-                    sums[l * 32] = 0.0f;
+                    v[l] = 0.0f;
+#pragma unroll
+                    for (int k = 0; k < LG_SETS; ++k) {
+                        v[l] += sums[(k * LIN_LEVELS + l) * 32];
+                        sums[(k * LIN_LEVELS + l) * 32] = 0.0f;
+                    }
                 }
                 if (have) {
                     float4 *out = reinterpret_cast<float4 *>(p.partial + ((static_cast<size_t>(u.part) * 2 + half) * p.d_out + j) * LIN_LEVELS);

@@ -217,8 +217,7 @@ __device__ __forceinline__ unsigned long long ld_cluster_u64(uint32_t addr)
 //
 // Alternatives: a thread keeps only the largest of its values.  Of 64 groups of threads, the top-th largest of the groups' largest
 // values is one that at least `top` entries reach, so every alternative is among the entries not below it, and those are with the
-// threads whose largest is not below it: about `top` threads, whose chunks are read again (from L2) by their warp, 32 chunks at a
-// time.  What is found there, hardly more than `top` entries, is put in order by counting who is above whom.  Where ties make more than SC_CANDIDATES of
+// threads whose largest is not below it: about `top` threads, whose chunks are read again (from L2) by all lanes of their warps.  What is found there, hardly more than `top` entries, is put in order by counting who is above whom.  Where ties make more than SC_CANDIDATES of
 // them (a row of equal logits), the row is gone through once for each alternative instead.
 //
 // Many rows: CTAs of 128 threads, so that an SM works on many rows at once and the joints between a row's end and the next one's
@@ -234,6 +233,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) token_logprobs_kernel
     __shared__ uint32_t group_best[SC_GROUPS];
     __shared__ unsigned long long found[SC_CANDIDATES];
     __shared__ unsigned long long chosen[SC_MAX_TOP];             // this CTA's alternatives
+    __shared__ uint8_t owners[WARPS][32];
     __shared__ uint32_t floor_key;
     __shared__ int n_found;
 
@@ -368,16 +368,28 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) token_logprobs_kernel
                 if (at < SC_CANDIDATES) found[at] = entry_of(x, j);
             }
         };
-        uint32_t hot = __ballot_sync(0xffffffffu, value_key(best) >= least);
-        while (hot) {
-            const int owner = __ffs(hot) - 1;
-            hot &= hot - 1;
-            const int first = c0 + warp * 32 + owner;
-            for (int i = first + lane * THREADS; i < c1; i += 32 * THREADS) {
-                float f[Row::PER];
-                Row::unpack(ld_once_16(row.chunk(i)), f);
+        // The chunks of the warp's threads that reach it, dealt to all its lanes, four loads of a lane at a time.
+        const bool hot = value_key(best) >= least;
+        const uint32_t who = __ballot_sync(0xffffffffu, hot);
+        if (hot) owners[warp][__popc(who & ((1u << lane) - 1u))] = static_cast<uint8_t>(lane);
+        __syncwarp();
+        const int each = (c1 - c0 + THREADS - 1) / THREADS, items = __popc(who) * each;
+        for (int i0 = lane; i0 < items; i0 += 128) {
+            uint4 v[4];
+            int at[4];
 #pragma unroll
-                for (int e = 0; e < Row::PER; ++e) offer(f[e], row.first_of(i) + e);
+            for (int q = 0; q < 4; ++q) {
+                const int i = i0 + 32 * q, o = i / each;
+                at[q] = i < items ? c0 + warp * 32 + owners[warp][o] + (i - o * each) * THREADS : c1;
+                if (at[q] < c1) v[q] = ld_once_16(row.chunk(at[q]));
+            }
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                if (at[q] >= c1) continue;
+                float f[Row::PER];
+                Row::unpack(v[q], f);
+#pragma unroll
+                for (int e = 0; e < Row::PER; ++e) offer(f[e], row.first_of(at[q]) + e);
             }
         }
         if (extra >= 0) offer(row.at(extra), extra);
