@@ -392,7 +392,7 @@ size_t gq_linear_codes_bytes(int64_t d_in, int64_t d_out);
  *   Y          [n, ld_y] of `dtype` (rules as for X)
  *   Z          [n, ld_z] of `dtype` or NULL: the pre-activation, rounded, for gq_linear_grad
  * Sums are fp32, everything behind them too, rounded once at the end.  Levels are finite; what stands behind d_in in codes and X is
- * not looked at.  One launch: up to 8 tokens on kernels that read the codes once at memory speed, more on tensor cores.
+ * not looked at.  One launch: up to 16 tokens on a kernel that reads the codes once, more on the tensor cores.
  * Results are bit-reproducible.
  */
 enum gq_activation { GQ_ACT_NONE = 0, GQ_ACT_RELU = 1, GQ_ACT_SILU = 2, GQ_ACT_GELU = 3 };
@@ -412,7 +412,7 @@ int32_t gq_linear(const void *X, int32_t dtype, int64_t n, int64_t d_in, int64_t
  *   X          as given to gq_linear; NULL where d_table is not asked for
  *   dX         [n, ld_dx] of `dtype` or NULL; d_table fp32 [d_out, m] or NULL; d_bias fp32 [d_out] or NULL
  *   workspace  at least gq_linear_grad_workspace_bytes(n, d_in, d_out) bytes, 1024-byte aligned; NULL where neither d_table nor d_bias
- *              is asked for
+ *              is asked for.  Nothing in it outlives the call; calls that may overlap on the GPU need one each
  * All matrices by the rules of gq_linear's X.  d_table and d_bias are overwritten (zero for n = 0).  Sums are fp32 on the tensor cores over
  * at most 1024 tokens at a time for d_table, partial sums are added in a fixed order: results are bit-reproducible.
  */

@@ -635,8 +635,13 @@ def gq_codebook_update(W: torch.Tensor, Q: torch.Tensor, m: int, H: torch.Tensor
     return codebook, W_hat
 
 
-def _empty(shape, stride, dtype, device) -> torch.Tensor:
-    """torch.empty for a contiguous tensor whose strides are given: half the host time of a call (2.6 us instead of 5.0)."""
+def _empty(shape, stride, dtype, device, stream=None) -> torch.Tensor:
+    """torch.empty for a contiguous tensor whose strides are given: half the host time of a call (2.6 us instead of 5.0).  A call that is
+    given a stream of its own gets memory of that stream: what the current stream has still to do with memory that was
+    freed on it must not meet the call's outputs."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return torch.empty_strided(shape, stride, dtype=dtype, device=device)
     return torch.empty_strided(shape, stride, dtype=dtype, device=device)
 
 
@@ -662,17 +667,17 @@ def gq_token_logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor] = No
     targets, the last two without alternatives."""
     code, n, vocab, ld = _logits(logits, "logits")
     dev, fp32 = logits.device, torch.float32
-    entropy, stats = _empty((n,), (1,), fp32, dev), _empty((n, 2), (2, 1), fp32, dev)
+    entropy, stats = _empty((n,), (1,), fp32, dev, stream), _empty((n, 2), (2, 1), fp32, dev, stream)
     logp = top_logp = top_ids = None
     t_ptr = lp_ptr = tl_ptr = ti_ptr = 0
     names, tensors = ("logits",), (logits,)
     if targets is not None:
         t_ptr = _vector(targets, (n,), torch.int64, "targets")
-        logp = _empty((n,), (1,), fp32, dev)
+        logp = _empty((n,), (1,), fp32, dev, stream)
         lp_ptr = logp.data_ptr()
         names, tensors = ("logits", "targets"), (logits, targets)
     if top > 0:
-        top_logp, top_ids = _empty((n, top), (top, 1), fp32, dev), _empty((n, top), (top, 1), torch.int32, dev)
+        top_logp, top_ids = _empty((n, top), (top, 1), fp32, dev, stream), _empty((n, top), (top, 1), torch.int32, dev, stream)
         tl_ptr, ti_ptr = top_logp.data_ptr(), top_ids.data_ptr()
     _call("gq_token_logprobs",
           (logits.data_ptr(), code, n, vocab, ld, t_ptr, top, lp_ptr, entropy.data_ptr(), stats.data_ptr(), tl_ptr, ti_ptr), stream, names, tensors)
@@ -687,7 +692,7 @@ def gq_token_logprobs_grad(logits: torch.Tensor, targets: Optional[torch.Tensor]
     code, n, vocab, ld = _logits(logits, "logits")
     names, tensors = ["logits", "stats"], [logits, stats]
     if d_logits is None:
-        d_logits, ld_d = _empty((n, vocab), (vocab, 1), logits.dtype, logits.device), vocab
+        d_logits, ld_d = _empty((n, vocab), (vocab, 1), logits.dtype, logits.device, stream), vocab
     else:
         _dev(d_logits, logits.dtype, "d_logits")
         d_n, d_vocab, ld_d = _rows(d_logits, "d_logits")
@@ -727,8 +732,9 @@ def gq_linear_pack(Q: torch.Tensor, codebook: torch.Tensor, dtype=torch.bfloat16
     d_out, d_in = Q.shape
     if codebook.dim() != 2 or codebook.shape[0] != d_out or not codebook.is_contiguous():
         raise ValueError("codebook must be a contiguous [d_out, m] tensor")
-    codes = torch.empty((d_out, (d_in + 31) // 32 * 16), dtype=torch.uint8, device=Q.device)
-    table = torch.empty((d_out, 16), dtype=dtype, device=Q.device)
+    width = (d_in + 31) // 32 * 16
+    codes = _empty((d_out, width), (width, 1), torch.uint8, Q.device, stream)
+    table = _empty((d_out, 16), (16, 1), dtype, Q.device, stream)
     _call("gq_linear_pack", (Q.data_ptr(), codebook.data_ptr(), codebook.shape[1], d_in, d_out, _DTYPE_CODES[dtype], codes.data_ptr(),
                              table.data_ptr()), stream, ("Q", "codebook"), (Q, codebook))
     return codes, table
@@ -769,7 +775,7 @@ def gq_linear(X: torch.Tensor, codes: torch.Tensor, table: torch.Tensor, m: int,
     names, tensors = ("X", "codes", "table"), (X, codes, table)
     b_ptr = r_ptr = z_ptr = ld_r = ld_z = 0
     if Y is None:
-        Y, ld_y = _empty((n, d_out), (d_out, 1), dtype, X.device), d_out
+        Y, ld_y = _empty((n, d_out), (d_out, 1), dtype, X.device, stream), d_out
         y_ptr = Y.data_ptr()
     else:
         y_ptr, ld_y = _matrix(Y, (n, d_out), dtype, "Y")
@@ -814,20 +820,20 @@ def gq_linear_grad(dY: torch.Tensor, X: torch.Tensor, codes: torch.Tensor, table
             raise ValueError("dZ is dY without an activation")
     else:
         if dZ is None:
-            dZ = _empty((n, d_out), (d_out, 1), dtype, dev)
+            dZ = _empty((n, d_out), (d_out, 1), dtype, dev, stream)
         dz_ptr, ld_dz = _matrix(dZ, (n, d_out), dtype, "dZ")
         names, tensors = names + ("dZ",), tensors + (dZ,)
     if dX is not None:
         dx_ptr, ld_dx = _matrix(dX, (n, d_in), dtype, "dX")
         names, tensors = names + ("dX",), tensors + (dX,)
     elif need_x:
-        dX, ld_dx = _empty((n, d_in), (d_in, 1), dtype, dev), d_in
+        dX, ld_dx = _empty((n, d_in), (d_in, 1), dtype, dev, stream), d_in
         dx_ptr = dX.data_ptr()
     if need_table:
-        d_table = _empty((d_out, max(m, 1)), (max(m, 1), 1), torch.float32, dev)
+        d_table = _empty((d_out, max(m, 1)), (max(m, 1), 1), torch.float32, dev, stream)
         dt_ptr = d_table.data_ptr()
     if need_bias:
-        d_bias = _empty((d_out,), (1,), torch.float32, dev)
+        d_bias = _empty((d_out,), (1,), torch.float32, dev, stream)
         db_ptr = d_bias.data_ptr()
     if workspace is not None:
         ws_ptr, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()

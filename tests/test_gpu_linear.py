@@ -314,3 +314,57 @@ def test_binding_refuses(dev):
         libgq.gq_linear_grad(torch.zeros(5, 32, device=dev, dtype=torch.bfloat16), X, codes, table, 4)
     with pytest.raises(ValueError, match="dZ"):
         libgq.gq_linear_grad(torch.zeros(5, 32, device=dev, dtype=torch.bfloat16), X, codes, table, 4, dZ=torch.zeros(5, 32, device=dev).bfloat16())
+
+
+@pytest.mark.parametrize("n", [3, 20])
+def test_rows_further_apart_than_32_bits(dev, n):
+    """Activations, residual and outputs 2^28 elements apart: the last of 20 rows starts 10 GB behind the first."""
+    ld, d_in, d_out, m = 1 << 28, 72, 64, 16
+    gen, Q, codebook, codes, table, W = layer(dev, d_in, d_out, m, torch.bfloat16, 6)
+    X = torch.randn(n, d_in, generator=gen, device=dev).bfloat16()
+    R = torch.randn(n, d_out, generator=gen, device=dev).bfloat16()
+
+    def far(t):
+        f = torch.empty((n - 1) * ld + t.shape[1], dtype=t.dtype, device=dev).as_strided(t.shape, (ld, 1))
+        return f.copy_(t)
+    Y, Z = far(R), far(R)
+    want_z = torch.empty_like(R)
+    want = libgq.gq_linear(X, codes, table, m, residual=R, Z=want_z, activation=libgq.GQ_ACT_SILU)
+    libgq.gq_linear(far(X), codes, table, m, residual=far(R), Y=Y, Z=Z, activation=libgq.GQ_ACT_SILU)
+    assert torch.equal(Y, want) and torch.equal(Z, want_z)
+    ws = libgq.alloc_workspace(libgq.gq_linear_grad_workspace_bytes(n, d_in, d_out), dev)
+    a = libgq.gq_linear_grad(R, X, codes, table, m, ws, Z=want_z, activation=libgq.GQ_ACT_SILU)
+    b = libgq.gq_linear_grad(far(R), far(X), codes, table, m, ws, Z=Z, activation=libgq.GQ_ACT_SILU, dZ=far(R), dX=far(X))
+    libgq.gq_check()
+    assert all(torch.equal(p, q) for p, q in zip(a, b))
+
+
+@pytest.mark.parametrize("n,d_in,d_out,m", [(17, 2048, 248, 16), (40, 4096, 512, 16), (33, 16384, 256, 8), (100, 1032, 3000, 16), (256, 8192, 264, 4),
+                                            (300, 2056, 520, 16), (150, 15320, 712, 4), (256, 512, 9472, 16)])
+def test_few_tiles_share_the_contraction(dev, n, d_in, d_out, m):
+    """Clusters of two, four and eight pairs, forward and backward (whose contraction is the other dimension)."""
+    check_forward(dev, n, d_in, d_out, m, torch.float16, libgq.GQ_ACT_GELU, True, True, 8)
+    check_backward(dev, n, d_out, d_in, m, torch.bfloat16, libgq.GQ_ACT_RELU, 8)
+
+
+def test_two_calls_at_once(dev):
+    """Calls on several streams, each with its own outputs and workspace, give what they give alone."""
+    m, act = 16, libgq.GQ_ACT_GELU
+    jobs = []
+    for i, (n, d_in, d_out) in enumerate([(2, 4096, 1024), (40, 2048, 512), (900, 1032, 1408)]):
+        gen, Q, codebook, codes, table, W = layer(dev, d_in, d_out, m, torch.bfloat16, i)
+        X = torch.randn(n, d_in, generator=gen, device=dev).bfloat16()
+        Z = torch.randn(n, d_out, generator=gen, device=dev).bfloat16()
+        ws = libgq.alloc_workspace(libgq.gq_linear_grad_workspace_bytes(n, d_in, d_out), dev)
+        jobs.append(lambda st=None, X=X, Z=Z, codes=codes, table=table, ws=ws: [libgq.gq_linear(X, codes, table, m, activation=act, stream=st)] + list(
+            libgq.gq_linear_grad(Z, X, codes, table, m, ws, Z=Z, activation=act, stream=st)))
+    want = [job() for job in jobs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in jobs]
+    got = []
+    for _ in range(4):
+        got += [(i, job(s)) for i, (job, s) in enumerate(zip(jobs, streams))]
+    torch.cuda.synchronize()
+    libgq.gq_check()
+    for i, outs in got:
+        assert all(torch.equal(a, b) for a, b in zip(outs, want[i]))

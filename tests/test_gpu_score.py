@@ -262,3 +262,30 @@ def test_binding_refuses(dev):
         libgq.gq_token_logprobs(x, top=33)
     with pytest.raises(ValueError, match="stats"):
         libgq.gq_token_logprobs_grad(x, t, torch.zeros(3, device=dev), None, torch.zeros(3, device=dev))
+
+
+def test_rows_further_apart_than_32_bits(dev):
+    """Three rows of bf16 logits 2^30 elements apart: the last one starts 4 GB behind the first."""
+    ld, vocab = 1 << 30, 3001
+    buf = torch.empty(2 * ld + vocab, dtype=torch.bfloat16, device=dev)
+    x = buf.as_strided((3, vocab), (ld, 1))
+    x.copy_(3 * torch.randn(3, vocab, device=dev))
+    t = torch.tensor([5, 3000, 17], device=dev)
+    logp, entropy, stats = check_scores(x, t, 5)
+    out = torch.empty_like(buf).as_strided((3, vocab), (ld, 1))
+    d = torch.ones(3, device=dev)
+    assert torch.equal(libgq.gq_token_logprobs_grad(x, t, stats, entropy, d, d, d_logits=out), libgq.gq_token_logprobs_grad(x.contiguous(), t, stats, entropy, d, d))
+
+
+def test_two_calls_at_once(dev):
+    xs = [make(dev, n, 40000, torch.float32, seed=n)[:2] for n in (3, 1500)]
+    want = [libgq.gq_token_logprobs(x, t, top=9) for x, t in xs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in xs]
+    got = [[] for _ in xs]
+    for _ in range(5):
+        for i, (s, (x, t)) in enumerate(zip(streams, xs)):
+            got[i].append(libgq.gq_token_logprobs(x, t, top=9, stream=s))
+    torch.cuda.synchronize()
+    for i in range(len(xs)):
+        assert all(torch.equal(a, b) for run in got[i] for a, b in zip(run, want[i]))
