@@ -108,6 +108,19 @@ struct LogitRow {
             return fmaxf(top, fmaxf(lo, hi));
         }
     }
+    // Values below FLOOR are raised to it before the exponentials (0 times -inf would be NaN, and far from zero the exponents' rounding is
+    // no longer small); NaNs stay.  That changes nothing where the largest value is above BORDER; elsewhere, and above CEILING, the sums are
+    // formed from differences.
+    static constexpr float FLOOR = DT == 1 ? -65504.0f : -200704.0f;
+    static constexpr float BORDER = DT == 1 ? -6.0e4f : -1.0e5f, CEILING = 1.0e5f;
+    static __device__ __forceinline__ uint32_t floored(uint32_t a)
+    {
+        uint32_t r;
+        if constexpr (DT == 0) asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(0xC844C844u));
+        else if constexpr (DT == 1) asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(0xFBFFFBFFu));      // the lowest finite one
+        else asm("max.NaN.f32 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(0xC8440000u));
+        return r;
+    }
     static __device__ __forceinline__ uint32_t pair_max(uint32_t a, uint32_t b)
     {
         uint32_t r;
@@ -250,21 +263,36 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) token_logprobs_kernel
     if (rank == 0 && tid < row.head) extra = tid;
     if (rank == ranks - 1 && tid >= 8 && tid - 8 < row.tail) extra = row.first_of(row.chunks) + tid - 8;
 
-    SoftStats st{-FLT_MAX, 0.0f, 0.0f};
-    float best = __uint_as_float(0xff800000u);                    // -inf
+    // Sums of 2^y and y 2^y with y = x log2 e - c: one multiply-add and one exponential a value.  c is the largest value so far times log2 e,
+    // rounded; what the rounding is off by is taken out once at the end.  (Subtracting the maximum first, and keeping -inf from the second
+    // sum value by value: nine instructions a logit instead of seven and a half; the issue slots were 77 % busy.)
+    const float minus_inf = __uint_as_float(0xff800000u);
+    float best = minus_inf, c_ref = Row::FLOOR * SC_LOG2E, sum = 0.0f, weighted = 0.0f;
     auto take = [&](const uint4 (&v)[4]) {
-        best = Row::largest(v, best);
-        if (best > st.m) st.raise(best);
+        const float now = Row::largest(v, best);
+        if (now > best) {
+            best = now;
+            const float c2 = fmaxf(now, Row::FLOOR) * SC_LOG2E, d = fmaxf(c_ref - c2, -1000.0f), f = exp2_fast(d);
+            weighted = f * fmaf(d, sum, weighted);
+            sum *= f;
+            c_ref = c2;
+        }
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
+            const uint4 w = make_uint4(Row::floored(v[q].x), Row::floored(v[q].y), Row::floored(v[q].z), Row::floored(v[q].w));
             float f[Row::PER];
-            Row::unpack(v[q], f);
+            Row::unpack(w, f);
 #pragma unroll
-            for (int e = 0; e < Row::PER; ++e) st.add(f[e]);
+            for (int e = 0; e < Row::PER; ++e) {
+                const float y = fmaf(f[e], SC_LOG2E, -c_ref), x2 = exp2_fast(y);
+                sum += x2;
+                weighted = fmaf(x2, y, weighted);
+            }
         }
     };
     // Four chunks at a time, the next four on their way while four are added up.
-    int c = c0 + tid;
+    const int c_own = c0 + tid;
+    int c = c_own;
     const int rounds = c < c1 ? (c1 - c + THREADS - 1) / THREADS : 0;       // chunks of this thread
     auto load = [&](uint4 (&v)[4]) {
 #pragma unroll
@@ -297,6 +325,24 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) token_logprobs_kernel
 #pragma unroll
         for (int q = 0; q < 4; ++q) v[q] = q < left ? ld_once_16(row.chunk(c + q * THREADS)) : make_uint4(none, none, none, none);
         take(v);
+    }
+    SoftStats st{-FLT_MAX, 0.0f, 0.0f};
+    if (best > Row::BORDER && best < Row::CEILING) {
+        const float off = fmaf(best, SC_LOG2E, -c_ref), f = exp2_fast(-off);
+        st = SoftStats{best, f * sum, f * fmaf(-off, sum, weighted)};
+    } else if (best == minus_inf) {
+        if (sum != sum) st.s = st.t = sum;                        // nothing but -inf and NaN
+    } else {
+        // far from zero: once more, from differences to the maximum
+        for (int i = c_own; i < c1; i += THREADS) {
+            float f[Row::PER];
+            Row::unpack(ld_once_16(row.chunk(i)), f);
+#pragma unroll
+            for (int e = 0; e < Row::PER; ++e) {
+                if (f[e] > st.m) st.raise(f[e]);
+                st.add(f[e]);
+            }
+        }
     }
     if (extra >= 0) {
         const float x = row.at(extra);
@@ -362,8 +408,9 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) token_logprobs_kernel
     if (alternatives) {
         __syncthreads();
         const uint32_t least = floor_key;
+        const float least_value = key_value(least);               // (at least -inf; a NaN is not above it)
         auto offer = [&](float x, int j) {
-            if (value_key(x) >= least) {
+            if (x >= least_value) {
                 const int at = atomicAdd(&n_found, 1);
                 if (at < SC_CANDIDATES) found[at] = entry_of(x, j);
             }

@@ -289,3 +289,22 @@ def test_two_calls_at_once(dev):
     torch.cuda.synchronize()
     for i in range(len(xs)):
         assert all(torch.equal(a, b) for run in got[i] for a, b in zip(run, want[i]))
+
+
+@pytest.mark.parametrize("dtype", sorted(DT))
+@pytest.mark.parametrize("n", [6, 1206])
+def test_values_next_to_the_ends_of_the_type(dev, dtype, n):
+    """Rows far from zero, up to the largest and down to the lowest finite values, with -inf beside them: only differences count."""
+    big = torch.finfo(DT[dtype]).max
+    x, t, gen = make(dev, n, 2000, DT[dtype], seed=n, spread=2.0)
+    base = torch.tensor([0.0, 3.0e4, -6.4e4, 1.0e3, -1.0e3, 6.0e4] if dtype == "fp16" else [0.0, 1.0e20, -1.0e29, 3.0e4, -2.0e31, 1.0e36], device=dev)
+    x += base.repeat(n // 6)[:, None].to(x.dtype)
+    x[1, ::3] = -INF
+    x[2, 1::2] = -INF
+    x[3, :1999] = -big
+    x[4, 5:] = -big
+    x[5, 7] = big
+    x[0, 100:] = -INF
+    t[0], t[1], t[2], t[3], t[4], t[5] = 5, 1, 0, 1999, 3, 7
+    _, entropy, stats = check_scores(x, t, 3)
+    check_gradient(x, t, stats, entropy, gen)
