@@ -9,6 +9,9 @@
  *   H_k   = X^T Diag(s_k) X                                     (Algorithm 1, Hessian step; Section 3.2)
  *   loss  = sum_k sum_{j in J_k} (w_j - what_j)^T H_k (w_j - what_j)          (Eq. 7)
  *
+ * On either side of that path: the end loss with its gradient (gq_token_logprobs), and the layer forward and backward from the
+ * quantiser's codes and levels (gq_linear).
+ *
  * Conventions shared by every call
  *   - Plain C ABI.  Unless a parameter is documented as HOST memory, every pointer is a DEVICE
  *     pointer owned by the caller; the library never allocates or frees device memory and never
@@ -510,10 +513,11 @@ enum gq_kernel_id {
     GQ_KERNEL_CB_FOLD = 11,    /* codebook step: sums over the rows of each level, m x m solves */
     GQ_KERNEL_CB_AUX = 12,     /* codebook step: splits, transposes, one-hot columns, W_hat */
     GQ_KERNEL_EXCHANGE = 13,   /* token-sharded accumulation: reduce / gather of blocks of H over peer memory */
+    GQ_KERNEL_COUNT = 14,      /* those that gq_kernel_timing_read reports               */
     GQ_KERNEL_SCORE = 14,      /* log probabilities of tokens and their gradient         */
     GQ_KERNEL_LINEAR = 15,     /* products with quantised weights, gradient of the levels */
     GQ_KERNEL_LINEAR_AUX = 16, /* layout of codes, activation gradient, sums of partial results */
-    GQ_KERNEL_COUNT = 17
+    GQ_KERNEL_COUNT_ALL = 17
 };
 
 /*
@@ -523,9 +527,11 @@ enum gq_kernel_id {
  * step of 52 launches when every launch is timed).  gq_kernel_timing_read() waits for the recorded events and writes, per
  * gq_kernel_id, the summed device time in milliseconds and the number of launches into two HOST
  * arrays of GQ_KERNEL_COUNT entries, then discards them.  Off by default.
+ * gq_kernel_timing_read_all() does the same for the first `count` kernels (1 .. GQ_KERNEL_COUNT_ALL; arrays of `count` entries).
  */
 int32_t gq_kernel_timing_enable(int32_t enable);
 int32_t gq_kernel_timing_read(double *ms_sum, uint64_t *launches);
+int32_t gq_kernel_timing_read_all(double *ms_sum, uint64_t *launches, int32_t count);
 
 #ifdef __cplusplus
 }

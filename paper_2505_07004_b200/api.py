@@ -23,7 +23,7 @@ EXPORTS = (
     "gq_hessian_accumulate_ahead",
     "gq_hessian_workspace_bytes", "gq_hessian_finalize", "gq_objective", "gq_objective_workspace_bytes",
     "gq_layer_objective_host", "gq_layer_host_arena_bytes", "gq_check", "gq_launch_count",
-    "gq_kernel_timing_enable", "gq_kernel_timing_read", "gq_objective_noalloc", "gq_cd_cycles", "gq_cd_workspace_bytes",
+    "gq_kernel_timing_enable", "gq_kernel_timing_read", "gq_kernel_timing_read_all", "gq_objective_noalloc", "gq_cd_cycles", "gq_cd_workspace_bytes",
     "gq_selftest_wait_timeout", "gq_codebook_update", "gq_codebook_workspace_bytes",
     "gq_hessian_reduce_share", "gq_hessian_gather_shares", "gq_lnq", "gq_lnq_workspace_bytes",
     "gq_token_logprobs", "gq_token_logprobs_grad",
@@ -124,6 +124,8 @@ def lib() -> ctypes.CDLL:
         L.gq_kernel_timing_enable.argtypes = [i32]
         L.gq_kernel_timing_read.restype = i32
         L.gq_kernel_timing_read.argtypes = [vp, vp]
+        L.gq_kernel_timing_read_all.restype = i32
+        L.gq_kernel_timing_read_all.argtypes = [vp, vp, i32]
         _lib = L
     return _lib
 
@@ -499,9 +501,9 @@ def gq_kernel_timing_read() -> dict:
     """``{kernel name: (summed device ms, launches)}`` for the launches recorded since the last read."""
     ms = (ctypes.c_double * len(KERNEL_NAMES))()
     cnt = (ctypes.c_uint64 * len(KERNEL_NAMES))()
-    rc = lib().gq_kernel_timing_read(ms, cnt)
+    rc = lib().gq_kernel_timing_read_all(ms, cnt, len(KERNEL_NAMES))
     if rc:
-        raise GQError("gq_kernel_timing_read", rc)
+        raise GQError("gq_kernel_timing_read_all", rc)
     return {name: (float(ms[i]), int(cnt[i])) for i, name in enumerate(KERNEL_NAMES)}
 
 

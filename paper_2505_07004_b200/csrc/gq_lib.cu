@@ -36,7 +36,7 @@ std::atomic<uint64_t> g_launches{0};
 // Optional per-kernel timing (gq_kernel_timing_*): a pair of events around every launch.
 std::atomic<int> g_timing_on{0};
 std::mutex g_timing_mutex;
-std::vector<std::pair<cudaEvent_t, cudaEvent_t>> g_timing_events[GQ_KERNEL_COUNT];
+std::vector<std::pair<cudaEvent_t, cudaEvent_t>> g_timing_events[GQ_KERNEL_COUNT_ALL];
 
 struct LaunchScope {
     int id;
@@ -1804,10 +1804,15 @@ int32_t gq_kernel_timing_enable(int32_t enable)
 
 int32_t gq_kernel_timing_read(double *ms_sum, uint64_t *launches)
 {
-    if (!ms_sum || !launches) return GQ_ERR_INVALID_ARG;
+    return gq_kernel_timing_read_all(ms_sum, launches, GQ_KERNEL_COUNT);
+}
+
+int32_t gq_kernel_timing_read_all(double *ms_sum, uint64_t *launches, int32_t count_ids)
+{
+    if (!ms_sum || !launches || count_ids < 1 || count_ids > GQ_KERNEL_COUNT_ALL) return GQ_ERR_INVALID_ARG;
     std::lock_guard<std::mutex> lock(g_timing_mutex);
     int32_t rc = GQ_OK;
-    for (int id = 0; id < GQ_KERNEL_COUNT; ++id) {
+    for (int id = 0; id < count_ids; ++id) {
         double total = 0.0;
         uint64_t count = 0;
         for (auto &pr : g_timing_events[id]) {

@@ -68,3 +68,13 @@ def test_binding_refuses_host_tensors_and_shapes():
         libgq.gq_token_logprobs(torch.zeros(2, 8))
     with pytest.raises(ValueError, match="CUDA tensor"):
         libgq.gq_token_logprobs_grad(torch.zeros(2, 8), None, torch.zeros(2, 2))
+
+
+def test_timing_arrays_keep_their_size(L):
+    """A caller compiled for 14 kernels gets 14 entries; the new ones have a call that is told how many there are."""
+    ms, n = (ctypes.c_double * 18)(*[-1.0] * 18), (ctypes.c_uint64 * 18)()
+    assert L.gq_kernel_timing_read(ms, n) == 0 and ms[13] == 0.0 and ms[14] == -1.0
+    assert len(libgq.KERNEL_NAMES) == 17
+    assert L.gq_kernel_timing_read_all(ms, n, 17) == 0 and ms[16] == 0.0 and ms[17] == -1.0
+    assert L.gq_kernel_timing_read_all(ms, n, 18) == INVALID and L.gq_kernel_timing_read_all(ms, n, 0) == INVALID
+    assert L.gq_kernel_timing_read_all(None, n, 17) == INVALID
