@@ -205,10 +205,12 @@ int32_t device_info(DeviceInfo **out)
         GQ_CUDA(cudaFuncSetAttribute(gq::linear_pair_kernel<true, true, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, gq::LP_SMEM_BYTES));
         GQ_CUDA(cudaFuncSetAttribute(gq::linear_pair_kernel<true, true, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, gq::LP_SMEM_BYTES));
         GQ_CUDA(cudaFuncSetAttribute(gq::linear_pair_kernel<true, true, true>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
-        GQ_CUDA(cudaFuncSetAttribute(gq::linear_token_kernel<true, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, gq::LT_SMEM_BYTES));
-        GQ_CUDA(cudaFuncSetAttribute(gq::linear_token_kernel<true, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, gq::LT_SMEM_BYTES));
-        GQ_CUDA(cudaFuncSetAttribute(gq::linear_token_kernel<false, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, gq::LT_SMEM_BYTES));
-        GQ_CUDA(cudaFuncSetAttribute(gq::linear_token_kernel<false, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, gq::LT_SMEM_BYTES));
+        GQ_CUDA(cudaFuncSetAttribute(gq::linear_token_kernel<true, 1, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, gq::LT_SMEM_BYTES));
+        GQ_CUDA(cudaFuncSetAttribute(gq::linear_token_kernel<true, 1, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, gq::LT_SMEM_BYTES));
+        GQ_CUDA(cudaFuncSetAttribute(gq::linear_token_kernel<true, 2, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, gq::LT_SMEM_BYTES));
+        GQ_CUDA(cudaFuncSetAttribute(gq::linear_token_kernel<false, 1, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, gq::LT_SMEM_BYTES));
+        GQ_CUDA(cudaFuncSetAttribute(gq::linear_token_kernel<false, 1, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, gq::LT_SMEM_BYTES));
+        GQ_CUDA(cudaFuncSetAttribute(gq::linear_token_kernel<false, 2, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, gq::LT_SMEM_BYTES));
         GQ_CUDA(cudaFuncSetAttribute(gq::linear_level_grad_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, gq::LG_SMEM_BYTES));
         GQ_CUDA(cudaFuncSetAttribute(gq::hessian_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                      gq::HS_SMEM_BYTES));
@@ -1606,9 +1608,8 @@ int32_t gq_linear(const void *X, int32_t dtype, int64_t n, int64_t d_in, int64_t
     p.Z = static_cast<uint16_t *>(Z);
     p.ld_z = ld_z;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    // 16 tokens: the few-tokens kernel reads X once per 16 channels and falls behind where that is much (us, few-tokens / tensor cores):
-    // 4096 x 4096 10.4 / 16.8, 4096 -> 11008 23 / 31, 28672 -> 8192 104 / 88; there with 9 tokens 72 / 87.
-    if (n > 2 * gq::LT_TOKENS || (n > gq::LT_TOKENS && n * d_in * d_out > (11ll << 28))) return linear_pair(false, p, dtype, X, ld_x, m, di, st);
+    // Up to 16 tokens, few-tokens kernel / tensor cores in us: 4096 x 4096 9.3 / 16.8, 4096 -> 11008 21 / 31, 28672 -> 8192 79 / 88.
+    if (n > 2 * gq::LT_TOKENS) return linear_pair(false, p, dtype, X, ld_x, m, di, st);
     p.X = static_cast<const uint16_t *>(X);
     p.ld_x = ld_x;
     // The contraction is split over CTAs while there are fewer of them than SMs and their warps keep a piece each.
@@ -1618,8 +1619,9 @@ int32_t gq_linear(const void *X, int32_t dtype, int64_t n, int64_t d_in, int64_t
     while (ranks < gq::LT_MAX_CLUSTER && groups * ranks < static_cast<unsigned>(di->sm_count) && pieces >= 2 * ranks * gq::LT_WARPS) ranks *= 2;
     {
         LaunchScope scope(GQ_KERNEL_LINEAR, st);
-        const auto kernel = n > gq::LT_TOKENS ? (p.bf16 ? gq::linear_token_kernel<true, 2> : gq::linear_token_kernel<false, 2>)
-                                              : (p.bf16 ? gq::linear_token_kernel<true, 1> : gq::linear_token_kernel<false, 1>);
+        const auto kernel = n > gq::LT_TOKENS ? (p.bf16 ? gq::linear_token_kernel<true, 2, true> : gq::linear_token_kernel<false, 2, true>)
+                          : n > 2 ? (p.bf16 ? gq::linear_token_kernel<true, 1, true> : gq::linear_token_kernel<false, 1, true>)
+                                  : (p.bf16 ? gq::linear_token_kernel<true, 1, false> : gq::linear_token_kernel<false, 1, false>);
         launch_cluster(kernel, ranks, dim3(groups * ranks), gq::LT_THREADS, gq::LT_SMEM_BYTES, st, p, static_cast<int>(ranks));
     }
     GQ_CUDA(cudaGetLastError());

@@ -43,6 +43,18 @@ __device__ __forceinline__ uint32_t pick_bytes(uint32_t a, uint32_t b, uint32_t 
     return r;
 }
 
+__device__ __forceinline__ uint32_t ld_u32(const void *p)
+{
+    uint32_t v;
+    asm volatile("ld.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint32_t ld_shared_4(uint32_t addr)
+{
+    uint32_t v;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+    return v;
+}
 __device__ __forceinline__ uint4 ld_shared_16(uint32_t addr)
 {
     uint4 v;
@@ -218,7 +230,8 @@ constexpr int LT_K = 128;                 // contraction indices a warp takes at
 constexpr int LT_MAX_CLUSTER = 8;
 constexpr int LT_AHEAD = 4;               // pieces of codes on their way to a warp
 constexpr int LT_TABLE_BYTES = 256 * 128;         // levels of all pairs of codes for 8 channels, a word per lane
-constexpr int LT_CODE_BYTES = 2 * 32 * 16;        // a piece of a warp's codes
+constexpr int LT_CODE_PITCH = 80;                 // a channel's 64 bytes of a piece: with 16 more, words t of all channels lie in different banks
+constexpr int LT_CODE_BYTES = LT_CHANNELS * LT_CODE_PITCH;      // a piece of a warp's codes
 constexpr int LT_SMEM_BYTES = 2 * LT_TABLE_BYTES + LT_WARPS * LT_AHEAD * LT_CODE_BYTES;
 
 template <bool BF16>
@@ -235,25 +248,28 @@ __device__ __forceinline__ void mma_m16n8k16(float (&c)[4], uint32_t a0, uint32_
 }
 
 // 16 channels per cluster of `ranks` CTAs, the contraction dealt to their warps in pieces of 128.  The order of the contraction indices
-// inside a piece is free as long as both operands share it: lane (g, t) of a quad takes the 32 codes 32 t .. 32 t + 31 of
-// channels g and g + 8 (16 bytes each) and token g's activations at the same place, four codes a product and lane, so that codes
-// are read 64 contiguous bytes a channel and nothing is exchanged between lanes.
+// inside a piece is free as long as both operands share it.  SPREAD: lane (g, t) of a quad takes the indices 32 q + 8 t .. + 7 for
+// q = 0 .. 3, of token g's activations 16 bytes each, next to those of the quad's other lanes, and of channels g and g + 8 one word of
+// codes each.  Otherwise it takes 32 indices in a row, 32 t .. 32 t + 31: the codes it has copied itself, and activations whose 16-byte
+// loads lie 64 bytes apart in a quad, twice the lines.  28672 -> 8192, SPREAD / not: one token 42.5 / 39.9 us, four 44.4 / 48.0, eight
+// 55 / 66; 4096 x 4096, one token 6.2 / 5.6.
 //
 // Lookups: a byte of codes names two levels, which stand side by side in a table of 256 words for the channel.  Every lane has its
 // own copy in its own bank (row = byte, word = lane: 32 KB for 8 channels), so 32 random bytes meet no conflicts: a load and two integer
 // instructions for two weights, where looking them up in registers takes more than five.
-template <bool BF16, int NT>
+template <bool BF16, int NT, bool SPREAD>
 __global__ void __launch_bounds__(LT_THREADS, 2) linear_token_kernel(const LinearParams p, int ranks)
 {
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     constexpr int TOKENS = NT * LT_TOKENS, X_AHEAD = 2 / NT;      // (pieces of activations in registers)
-    __shared__ float sums[LT_WARPS][TOKENS][LT_CHANNELS];
+    constexpr int PITCH = SPREAD ? LT_CODE_PITCH : 64;            // of a channel's codes in shared memory
     __shared__ float mine[TOKENS * LT_CHANNELS];
     __shared__ uint16_t levels[LT_CHANNELS][LIN_LEVELS];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
     const int group = static_cast<int>(blockIdx.x) / ranks, rank = static_cast<int>(blockIdx.x) - group * ranks;
     const int j0 = group * LT_CHANNELS;
-    const uint32_t tables = smem_u32(smem_raw), ring = tables + 2 * LT_TABLE_BYTES + static_cast<uint32_t>(warp * LT_AHEAD * LT_CODE_BYTES + lane * 16);
+    const uint32_t tables = smem_u32(smem_raw), ring = tables + 2 * LT_TABLE_BYTES + static_cast<uint32_t>(warp * LT_AHEAD * LT_CODE_BYTES);
+    float (*sums)[TOKENS][LT_CHANNELS] = reinterpret_cast<float (*)[TOKENS][LT_CHANNELS]>(smem_raw + 2 * LT_TABLE_BYTES);      // after the ring's use
     griddep_launch();
     griddep_wait();
     // channels are a multiple of 8, so either all of g or all of g + 8 are there
@@ -270,14 +286,15 @@ __global__ void __launch_bounds__(LT_THREADS, 2) linear_token_kernel(const Linea
     const int pieces = (p.d_in + LT_K - 1) / LT_K, stride = ranks * LT_WARPS;
     // A warp takes pairs of neighbouring pieces (128 bytes of a channel's codes): pairs base, base + stride, ...  The `whole` first of its pieces
     // lie inside the row, one ragged piece may follow.
-    // Codes come from device memory, by asynchronous copies LT_AHEAD pieces ahead: each lane copies and reads its own 16 bytes, so nothing but
-    // its own wait is needed; in registers the loads of four pieces shared the few scoreboards there are, and waits for one waited
-    // for the others.  Activations come from L2 or L1, one or two pieces ahead, in registers.
+    // Codes come from device memory, by asynchronous copies LT_AHEAD pieces ahead, 16 bytes of either channel a lane; in registers the loads
+    // of four pieces shared the few scoreboards there are, and waits for one waited for the others.  Activations come from L2 or L1, one or two pieces ahead, in registers.
     const int base = rank * LT_WARPS + warp, full = p.d_in / LT_K, last_pair = full / 2;
     const int whole = (base < last_pair ? 2 * ((last_pair - base + stride - 1) / stride) : 0) + ((full & 1) != 0 && last_pair % stride == base ? 1 : 0);
     const bool ragged = full < pieces && last_pair % stride == base;
-    // contraction index of the i-th piece, for this lane
-    auto index_of = [&](int i) { return ((base + (i >> 1) * stride) * 2 + (i & 1)) * LT_K + 32 * t; };
+    auto index_of = [&](int i) { return ((base + (i >> 1) * stride) * 2 + (i & 1)) * LT_K; };      // first index of the i-th piece
+    auto eight = [&](int q) { return SPREAD ? 32 * q + 8 * t : 32 * t + 8 * q; };              // this lane's q-th eight indices in a piece
+    const uint32_t copy_to = ring + static_cast<uint32_t>(g * PITCH + t * 16), word_at = ring + static_cast<uint32_t>(g * PITCH + t * 4);
+    constexpr uint32_t SECOND = 8 * PITCH;                      // channels 8 .. 15
     uint4 tokens[X_AHEAD][NT][4];
 #pragma unroll
     for (int d = 0; d < X_AHEAD; ++d)
@@ -287,9 +304,9 @@ __global__ void __launch_bounds__(LT_THREADS, 2) linear_token_kernel(const Linea
             for (int q = 0; q < 4; ++q) tokens[d][o][q] = make_uint4(0u, 0u, 0u, 0u);      // stays so in lanes without a token
     auto fetch_codes = [&](int i, int slot) {
         if (i < whole) {
-            const int at = index_of(i) >> 1;
-            copy_async_16(ring + slot * LT_CODE_BYTES, ca + at);
-            copy_async_16(ring + slot * LT_CODE_BYTES + LT_CODE_BYTES / 2, cb + at);
+            const int at = (index_of(i) >> 1) + 16 * t;
+            copy_async_16(copy_to + slot * LT_CODE_BYTES, ca + at);
+            copy_async_16(copy_to + slot * LT_CODE_BYTES + SECOND, cb + at);
         }
         copy_async_commit();                                     // a group a piece, empty past the end
     };
@@ -298,7 +315,7 @@ __global__ void __launch_bounds__(LT_THREADS, 2) linear_token_kernel(const Linea
         for (int o = 0; o < NT; ++o)
             if (i < whole && have[o]) {
 #pragma unroll
-                for (int q = 0; q < 4; ++q) f[o][q] = ld_u32x4(x[o] + index_of(i) + 8 * q);
+                for (int q = 0; q < 4; ++q) f[o][q] = ld_u32x4(x[o] + index_of(i) + eight(q));
             }
     };
 #pragma unroll
@@ -330,8 +347,7 @@ __global__ void __launch_bounds__(LT_THREADS, 2) linear_token_kernel(const Linea
         const uint32_t at = ((byte == 0 ? w << 7 : w >> (8 * byte - 7)) & 0x7F80u) | static_cast<uint32_t>(lane * 4);
         return *reinterpret_cast<const uint32_t *>(smem_raw + table * LT_TABLE_BYTES + at);
     };
-    auto use = [&](const uint4 (&f)[2], const uint4 (&y)[NT][4], int end) {
-        const uint32_t qa[4] = {f[0].x, f[0].y, f[0].z, f[0].w}, qb[4] = {f[1].x, f[1].y, f[1].z, f[1].w};
+    auto use = [&](const uint32_t (&qa)[4], const uint32_t (&qb)[4], const uint4 (&y)[NT][4], int end) {
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             uint32_t wa[4], wb[4];
@@ -340,7 +356,7 @@ __global__ void __launch_bounds__(LT_THREADS, 2) linear_token_kernel(const Linea
                 wa[e] = word(0, qa[q], e);
                 wb[e] = word(1, qb[q], e);
             }
-            if (8 * q >= end) {                                       // (never in a whole piece) no level meets padding
+            if (eight(q) >= end) {                                    // (never in a whole piece) no level meets padding
 #pragma unroll
                 for (int e = 0; e < 4; ++e) wa[e] = wb[e] = 0u;
             }
@@ -356,25 +372,40 @@ __global__ void __launch_bounds__(LT_THREADS, 2) linear_token_kernel(const Linea
         for (int d = 0; d < LT_AHEAD; ++d) {
             if (i + d >= whole) break;
             copy_async_wait<LT_AHEAD - 1>();
-            const uint4 f[2] = {ld_shared_16(ring + d * LT_CODE_BYTES), ld_shared_16(ring + d * LT_CODE_BYTES + LT_CODE_BYTES / 2)};
-            use(f, tokens[d % X_AHEAD], LT_K);
-            fetch_codes(i + d + LT_AHEAD, d);                    // into what has been read and used
+            uint32_t qa[4], qb[4];
+            if (SPREAD) {
+                __syncwarp();                                    // the other lanes' copies
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    qa[q] = ld_shared_4(word_at + d * LT_CODE_BYTES + 16 * q);
+                    qb[q] = ld_shared_4(word_at + d * LT_CODE_BYTES + SECOND + 16 * q);
+                }
+            } else {
+                const uint4 a = ld_shared_16(copy_to + d * LT_CODE_BYTES), b = ld_shared_16(copy_to + d * LT_CODE_BYTES + SECOND);
+                qa[0] = a.x, qa[1] = a.y, qa[2] = a.z, qa[3] = a.w;
+                qb[0] = b.x, qb[1] = b.y, qb[2] = b.z, qb[3] = b.w;
+            }
+            use(qa, qb, tokens[d % X_AHEAD], LT_K);
+            if (SPREAD) __syncwarp();                            // all lanes have read
+            fetch_codes(i + d + LT_AHEAD, d);
             fetch_tokens(i + d + X_AHEAD, tokens[d % X_AHEAD]);
         }
     }
     if (ragged) {
-        const int k = full * LT_K + 32 * t;
-        uint4 f[2] = {make_uint4(0u, 0u, 0u, 0u), make_uint4(0u, 0u, 0u, 0u)}, y[NT][4];
-        if (k < p.d_in) {
-            f[0] = ld_once_16(reinterpret_cast<const uint4 *>(ca + (k >> 1)));
-            f[1] = ld_once_16(reinterpret_cast<const uint4 *>(cb + (k >> 1)));
+        uint32_t qa[4], qb[4];
+        uint4 y[NT][4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int k = full * LT_K + eight(q);
+            const bool in = k < p.d_in;
+            qa[q] = in ? ld_u32(ca + (k >> 1)) : 0u;
+            qb[q] = in ? ld_u32(cb + (k >> 1)) : 0u;
+#pragma unroll
+            for (int o = 0; o < NT; ++o) y[o][q] = in && have[o] ? ld_u32x4(x[o] + k) : make_uint4(0u, 0u, 0u, 0u);
         }
-#pragma unroll
-        for (int o = 0; o < NT; ++o)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) y[o][q] = (have[o] && k + 8 * q < p.d_in) ? ld_u32x4(x[o] + k + 8 * q) : make_uint4(0u, 0u, 0u, 0u);
-        use(f, y, p.d_in - k);
+        use(qa, qb, y, p.d_in - full * LT_K);
     }
+    __syncthreads();                                             // the ring has been read: the sums take its place
     // c[0], c[1]: channel g, tokens 2 t, 2 t + 1; c[2], c[3]: channel g + 8
 #pragma unroll
     for (int o = 0; o < NT; ++o)
