@@ -104,7 +104,7 @@ void launch_cluster(void (*kernel)(Params...), unsigned ranks, dim3 grid, int th
     attr[1].val.clusterDim.y = 1;
     attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 2;
+    cfg.numAttrs = ranks > 1 ? 2 : 1;
     (void)cudaLaunchKernelEx(&cfg, kernel, static_cast<Params>(args)...);
 }
 
