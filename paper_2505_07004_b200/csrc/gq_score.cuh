@@ -230,7 +230,8 @@ __device__ __forceinline__ unsigned long long ld_cluster_u64(uint32_t addr)
 //
 // Alternatives: a thread keeps only the largest of its values.  Of 64 groups of threads, the top-th largest of the groups' largest
 // values is one that at least `top` entries reach, so every alternative is among the entries not below it, and those are with the
-// threads whose largest is not below it: about `top` threads, whose chunks are read again (from L2) by all lanes of their warps.  What is found there, hardly more than `top` entries, is put in order by counting who is above whom.  Where ties make more than SC_CANDIDATES of
+// threads whose largest is not below it: about `top` threads, of which the four chunks with the largest value are read again (from L2), or all where the others
+// reach it too.  What is found there, hardly more than `top` entries, is put in order by counting who is above whom.  Where ties make more than SC_CANDIDATES of
 // them (a row of equal logits), the row is gone through once for each alternative instead.
 //
 // Many rows: CTAs of 128 threads, so that an SM works on many rows at once and the joints between a row's end and the next one's
@@ -246,7 +247,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) token_logprobs_kernel
     __shared__ uint32_t group_best[SC_GROUPS];
     __shared__ unsigned long long found[SC_CANDIDATES];
     __shared__ unsigned long long chosen[SC_MAX_TOP];             // this CTA's alternatives
-    __shared__ uint8_t owners[WARPS][32];
+    __shared__ int owners[WARPS][32];                             // first chunks to search
     __shared__ uint32_t floor_key;
     __shared__ int n_found;
 
@@ -268,15 +269,23 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) token_logprobs_kernel
     // sum value by value: nine instructions a logit instead of seven and a half; the issue slots were 77 % busy.)
     const float minus_inf = __uint_as_float(0xff800000u);
     float best = minus_inf, c_ref = Row::FLOOR * SC_LOG2E, sum = 0.0f, weighted = 0.0f;
+    // (for the alternatives: the four chunks with the largest value, and the largest value of all others)
+    float second = minus_inf;
+    int where = 0, batch = 0;
     auto take = [&](const uint4 (&v)[4]) {
-        const float now = Row::largest(v, best);
-        if (now > best) {
+        const float now = Row::largest(v, minus_inf);
+        if (now <= best) {
+            second = fmaxf(second, now);
+        } else if (now > best) {
+            second = best;
+            where = batch;
             best = now;
             const float c2 = fmaxf(now, Row::FLOOR) * SC_LOG2E, d = fmaxf(c_ref - c2, -1000.0f), f = exp2_fast(d);
             weighted = f * fmaf(d, sum, weighted);
             sum *= f;
             c_ref = c2;
         }
+        ++batch;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             const uint4 w = make_uint4(Row::floored(v[q].x), Row::floored(v[q].y), Row::floored(v[q].z), Row::floored(v[q].w));
@@ -326,6 +335,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) token_logprobs_kernel
         for (int q = 0; q < 4; ++q) v[q] = q < left ? ld_once_16(row.chunk(c + q * THREADS)) : make_uint4(none, none, none, none);
         take(v);
     }
+    const float best_chunk = best;
     SoftStats st{-FLT_MAX, 0.0f, 0.0f};
     if (best > Row::BORDER && best < Row::CEILING) {
         const float off = fmaf(best, SC_LOG2E, -c_ref), f = exp2_fast(-off);
@@ -415,30 +425,39 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) token_logprobs_kernel
                 if (at < SC_CANDIDATES) found[at] = entry_of(x, j);
             }
         };
-        // The chunks of the warp's threads that reach it, dealt to all its lanes, four loads of a lane at a time.
-        const bool hot = value_key(best) >= least;
-        const uint32_t who = __ballot_sync(0xffffffffu, hot);
-        if (hot) owners[warp][__popc(who & ((1u << lane) - 1u))] = static_cast<uint8_t>(lane);
+        // The chunks that may reach it, dealt to all lanes of the warp, four loads of a lane at a time: of a thread whose other chunks stay below
+        // it the four with its largest value, of the others all.
+        const bool hot = value_key(best_chunk) >= least, wide = hot && second >= least_value;
+        const int each = (c1 - c0 + THREADS - 1) / THREADS;
+        auto search = [&](uint32_t who, int count) {              // `count` chunks of each of these threads, from the one it has named
+            const int items = __popc(who) * count;
+            for (int i0 = lane; i0 < items; i0 += 128) {
+                uint4 v[4];
+                int at[4];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int i = i0 + 32 * q, o = i / count;
+                    at[q] = i < items ? owners[warp][o] + (i - o * count) * THREADS : c1;
+                    if (at[q] < c1) v[q] = ld_once_16(row.chunk(at[q]));
+                }
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    if (at[q] >= c1) continue;
+                    float f[Row::PER];
+                    Row::unpack(v[q], f);
+#pragma unroll
+                    for (int e = 0; e < Row::PER; ++e) offer(f[e], row.first_of(at[q]) + e);
+                }
+            }
+            __syncwarp();
+        };
+        const uint32_t below = (1u << lane) - 1u, some = __ballot_sync(0xffffffffu, hot && !wide), all = __ballot_sync(0xffffffffu, wide);
+        if (hot && !wide) owners[warp][__popc(some & below)] = c_own + 4 * where * THREADS;
         __syncwarp();
-        const int each = (c1 - c0 + THREADS - 1) / THREADS, items = __popc(who) * each;
-        for (int i0 = lane; i0 < items; i0 += 128) {
-            uint4 v[4];
-            int at[4];
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int i = i0 + 32 * q, o = i / each;
-                at[q] = i < items ? c0 + warp * 32 + owners[warp][o] + (i - o * each) * THREADS : c1;
-                if (at[q] < c1) v[q] = ld_once_16(row.chunk(at[q]));
-            }
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                if (at[q] >= c1) continue;
-                float f[Row::PER];
-                Row::unpack(v[q], f);
-#pragma unroll
-                for (int e = 0; e < Row::PER; ++e) offer(f[e], row.first_of(at[q]) + e);
-            }
-        }
+        search(some, 4);
+        if (wide) owners[warp][__popc(all & below)] = c_own;
+        __syncwarp();
+        search(all, each);
         if (extra >= 0) offer(row.at(extra), extra);
         __syncthreads();
         const int count = n_found;
