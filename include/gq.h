@@ -362,7 +362,7 @@ int32_t gq_token_logprobs(const void *logits, int32_t dtype, int64_t n, int64_t 
  *   d_logp     fp32 [n] or NULL (with targets); d_entropy fp32 [n] or NULL (entropy may then be NULL); one of them is given
  *   d_logits   [n, ld_d] of `dtype`, aligned to its element size, ld_d >= vocab, rounded once at the end
  * Rows whose token does not count, or with d_logp = 0, and without an entropy gradient get zeros whatever their logits hold;
- * so does a row of nothing but -inf.
+ * so does a row of nothing but -inf.  Probabilities below 2^-126 are 0.
  */
 int32_t gq_token_logprobs_grad(const void *logits, int32_t dtype, int64_t n, int64_t vocab, int64_t ld, const int64_t *targets,
                                const float *stats, const float *entropy, const float *d_logp, const float *d_entropy,

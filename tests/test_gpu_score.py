@@ -163,11 +163,13 @@ def check_gradient(x, t, stats, entropy, gen, with_logp=True, with_entropy=True,
     hit.scatter_(1, torch.where(counted, t, 0)[:, None], 1.0)
     want = w * (hit * counted[:, None] - p) - h * (torch.special.xlogy(p, p) + p * entropy.double()[:, None])
     want = torch.where(none, 0.0, want)
-    # two subtractions, a product and the exponential give p to (2 |x - m| + 2 L + 4) u; the sums of products a few u more
+    # two subtractions, a product and the exponential give p to (2 |x - m| + 2 L + 4) u; the sums of products a few u more; a p below
+    # 2^-126 is taken as 0
     bend = torch.where(p > 0, (2 * (xd - sd[:, :1]).abs() + 2 * sd[:, 1:] + 8) * U, 0.0)
     size = p * (w.abs() + h.abs() * (logp.clamp_min(-200.0).abs() + entropy.double()[:, None].abs()))
     size = torch.where(none, 0.0, size)
-    tol = 2 * bend * size + 4 * U * (size + w.abs() * hit) + want.abs() * (torch.finfo(x.dtype).eps / 2)
+    lost = torch.where(p < 2.0 ** -126, size, 0.0)
+    tol = lost + 2 * bend * size + 4 * U * (size + w.abs() * hit) + want.abs() * (torch.finfo(x.dtype).eps / 2)
     tol = tol + (torch.finfo(x.dtype).smallest_normal * torch.finfo(x.dtype).eps if x.dtype != torch.float32 else 2.0 ** -126)
     tol = tol * 1.01
     assert bool(((got.double() - want).abs() <= tol).all()), ((got.double() - want).abs() / tol).max().item()
