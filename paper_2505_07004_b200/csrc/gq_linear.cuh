@@ -6,11 +6,12 @@
 // Layout (linear_pack_kernel): codes [d_out][ld] bytes, two codes a byte, the lower four bits first, ld = 16 ceil(d_in / 32);
 // table [d_out][16] in the activations' type (bf16 or fp16), zero from m on.
 //
-// On the tensor cores' path a level is looked up in registers: a channel's 16 levels are kept as two planes of 16 bytes (low and high bytes, eight
-// registers), and a byte permutation looks four codes up in eight bytes at once.  For four weights: two permutations a plane (levels
-// 0..7 and 8..15), one that takes either by the codes' top bits, and two that join the planes: 2.6 integer instructions a weight, 1.3
-// where m <= 8.  Few tokens (linear_token_kernel, n <= 8) are bound by the codes' bytes and, behind them, the lookups, and use tables in
-// shared memory.  More tokens (linear_pair_kernel): tensor cores, the weight operand written to shared memory by eight lookup warps.
+// On the tensor cores' path a level is looked up in registers: a channel's 16 levels are kept as two planes of 16 bytes (low and high
+// bytes, eight registers), and a byte permutation looks four codes up in eight bytes at once.  For four weights: two permutations a
+// plane (levels 0..7 and 8..15), one that takes either by the codes' top bits, and two that join the planes: 2.6 integer instructions a
+// weight, 1.3 where m <= 8.  Few tokens (linear_token_kernel, up to 16) are bound by the codes' bytes and, behind them, the lookups,
+// and use tables in shared memory.  More tokens (linear_pair_kernel): tensor cores, the weight operand written to shared memory by
+// eight lookup warps.
 #pragma once
 #include <cuda.h>
 #include <cuda_bf16.h>
@@ -287,7 +288,8 @@ __global__ void __launch_bounds__(LT_THREADS, 2) linear_token_kernel(const Linea
     // A warp takes pairs of neighbouring pieces (128 bytes of a channel's codes): pairs base, base + stride, ...  The `whole` first of its pieces
     // lie inside the row, one ragged piece may follow.
     // Codes come from device memory, by asynchronous copies LT_AHEAD pieces ahead, 16 bytes of either channel a lane; in registers the loads
-    // of four pieces shared the few scoreboards there are, and waits for one waited for the others.  Activations come from L2 or L1, one or two pieces ahead, in registers.
+    // of four pieces shared the few scoreboards there are, and waits for one waited for the others (one token 44 us instead of 39).
+    // Activations come from L2 or L1, one or two pieces ahead, in registers.
     const int base = rank * LT_WARPS + warp, full = p.d_in / LT_K, last_pair = full / 2;
     const int whole = (base < last_pair ? 2 * ((last_pair - base + stride - 1) / stride) : 0) + ((full & 1) != 0 && last_pair % stride == base ? 1 : 0);
     const bool ragged = full < pieces && last_pair % stride == base;
@@ -551,13 +553,14 @@ __device__ __forceinline__ bool linear_unit(const LinearParams &p, int pair, int
 // owns a channel for the whole tile, its levels stay in registers.  Backward: D[c][token] = sum_j W[j][c] dZ[token][j]; the rows of
 // the weight operand are contraction indices, a lookup thread owns 64 columns of one channel a k-step and reads that channel's levels
 // a step ahead.  Codes come by TMA as well, those of four k-steps together: read by the lookup threads from global memory they cost
-// 28 us of 313 (8192 x 4096 x 4096), and boxes of 128 rows of 32 bytes, a k-step each, came once in 850 clocks.  A looked-up operand serves two tiles of 256 tokens, the two accumulators that tensor memory
-// holds: with one tile each, lookups and their stores were in the way of the tensor core (263 us, 221 with the lookups left out).
+// 28 us of 313 (8192 x 4096 x 4096); with two k-steps a box 32 tokens of 28672 -> 8192 take 95 us instead of 88.  A looked-up
+// operand serves two tiles of 256 tokens, the two accumulators that tensor memory holds: with one tile each, lookups and their stores
+// were in the way of the tensor core (263 us, 221 with the lookups left out; now 182, 1.5 PFLOP/s).
 // Rows of D are the lanes of tensor memory, so tokens (columns) come in any number without work for the weights' side.
 //
 // SPLIT: few tiles.  A cluster of `ranks` pairs works on one tile of 256 rows and up to 256 tokens, a share of the contraction each; the
 // partial sums go to shared memory (where the ring was) and every pair joins a share of the tokens through distributed shared memory.
-// 77 tokens, 1032 -> 3000: 12 pairs instead of one tile each on 12 of 74.
+// 64 tokens of 4096 x 4096, 16 tiles: 53 us on as many pairs when this was built, 31 on twice as many; 18 now.
 template <bool BACK, bool WIDE, bool SPLIT>
 __global__ void __launch_bounds__(LP_THREADS, 1)
 linear_pair_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_constant__ CUtensorMap mapC, const LinearParams p)
