@@ -1390,11 +1390,13 @@ int32_t gq_token_logprobs(const void *logits, int32_t dtype, int64_t n, int64_t 
     if (int32_t rc = check_disjoint(wr, ro)) return rc;
     DeviceInfo *di;
     if (int32_t rc = device_info(&di)) return rc;
-    // Rows for eight CTAs of 128 threads on every SM: such CTAs, one a row.  Otherwise 512 threads, and rows are split while there are fewer
-    // CTAs than SMs and a CTA keeps a round of 16-byte loads.
-    const bool narrow = n >= 8 * static_cast<int64_t>(di->sm_count);
-    unsigned ranks = 1;
+    // Rows for four CTAs of 128 threads on every SM, or short ones (a round of loads each): such CTAs, one a row.  512 / 128 threads in us:
+    // 1100 x 2000 bf16 with 20 alternatives 22.1 / 8.8, 400 x 1000 with five 9.4 / 5.8, 725 x 22982 14.8 / 12.1, 600 x 128000 fp32 54.0 / 50.8;
+    // 300 x 128000 bf16 19.3 / 23.4.  Otherwise 512 threads, and rows are split while there are fewer CTAs than SMs and a CTA keeps a
+    // round of 16-byte loads.
     const int64_t chunks = vocab * static_cast<int64_t>(dtype_bytes(dtype)) / 16;
+    const bool narrow = n >= 4 * static_cast<int64_t>(di->sm_count) || chunks <= 4 * gq::SC_NARROW;
+    unsigned ranks = 1;
     while (!narrow && ranks < gq::SC_MAX_CLUSTER && n * ranks < di->sm_count && chunks >= 2 * ranks * gq::SC_WIDE) ranks *= 2;
     gq::ScoreParams p{};
     p.logits = logits;
