@@ -18,8 +18,8 @@
 
 namespace gq {
 
-constexpr int SC_WIDE = 512;             // threads of a CTA where rows are few
-constexpr int SC_NARROW = 128;           // and where there are many
+constexpr int SC_WIDE = 512;             // threads of a CTA where rows are few and long
+constexpr int SC_NARROW = 128;           // and where they are many or short
 constexpr int SC_GROUPS = 64;            // groups of threads whose largest values bound the alternatives from below
 constexpr int SC_MAX_TOP = 32;
 constexpr int SC_MAX_CLUSTER = 8;
@@ -235,8 +235,8 @@ __device__ __forceinline__ unsigned long long ld_cluster_u64(uint32_t addr)
 // in order by counting who is above whom.  Where ties make more than SC_CANDIDATES of them (a row of equal logits), the row is gone
 // through once for each alternative instead.  4096 x 32000 bf16: 48 us, with 20 alternatives 81.
 //
-// Many rows: CTAs of 128 threads, so that an SM works on many rows at once and the joints between a row's end and the next one's
-// beginning are covered; 4096 x 32000 bf16 took 80 us with 512 threads a row.
+// Many rows or short ones: CTAs of 128 threads, so that an SM works on many rows at once and the joints between a row's end and the
+// next one's beginning are covered; 4096 x 32000 bf16 took 80 us with 512 threads a row.
 template <int DT, int THREADS>
 __global__ void __launch_bounds__(THREADS, 1024 / THREADS) token_logprobs_kernel(const ScoreParams p, int ranks)
 {
