@@ -127,26 +127,17 @@ __device__ __forceinline__ void activate(float (&z)[N], int act)
         for (int e = 0; e < N; ++e) z[e] = 0.5f * z[e] * (1.0f + erff(z[e] * 0.70710678118654752f));
     }
 }
-// 1 / (1 + exp(-z)) to two or three units in the last place: the exponent -z log2 e in two terms, a Newton step on the reciprocal.  Half the
-// instructions of the library's exponential and division, behind which the activation gradient of 2048 x 4096 took 20 us.
-__device__ __forceinline__ float sigmoid(float z)
-{
-    const float t = fminf(z * -SC_LOG2E, 126.0f);
-    const float rest = fmaf(z, -SC_LOG2E, -t) + z * -1.9259629911266175e-8f;      // log2 e = SC_LOG2E + 1.926e-8
-    float e = exp2_fast(t);
-    e = fmaf(e, t == 126.0f ? 0.0f : rest * SC_LN2, e);
-    const float d = 1.0f + e;
-    float r;
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(d));
-    return fmaf(r, fmaf(-d, r, 1.0f), r);
-}
 // The slope's fp32 value decides how dZ is rounded, and the fp32 gradients are those of the rounded dZ: no fast approximations.
+// SiLU: s (1 + z (1 - s)) with s = 1 / (1 + exp(-z)).  From e = exp(-|z|) <= 1 both s and 1 - s follow without a difference, 1 / (1 + e) and
+// e / (1 + e) or the other way round; the divisor lies in [1, 2], and where e is 0 the slope is 0 or 1, whatever z is.  To 24 times 2^-24 of
+// s (1 + |z| (1 - s)).
 __device__ __forceinline__ float activation_slope(float z, int act)
 {
     if (act == LIN_RELU) return z > 0.0f ? 1.0f : 0.0f;
     if (act == LIN_SILU) {
-        const float sig = sigmoid(z);
-        return sig * (1.0f + z * (1.0f - sig));
+        const float e = expf(-fabsf(z)), near = __fdividef(1.0f, 1.0f + e), far = e * near;
+        const float s = z < 0.0f ? far : near, rest = z < 0.0f ? near : far;
+        return s * fmaf(z, rest, 1.0f);
     }
     if (act == LIN_GELU) return 0.5f * (1.0f + erff(z * 0.70710678118654752f)) + z * expf(-0.5f * z * z) * 0.39894228040143268f;
     return 1.0f;
