@@ -1233,8 +1233,14 @@ linear_level_grad_kernel(const __grid_constant__ CUtensorMap mapG, const __grid_
                     if (lane == 0) mbar_arrive_cluster(map_to_cta(smem_u32(&bar_acc_empty[buf]), 0));
                 }
                 const uint32_t w[4] = {codes[x].x, codes[x].y, codes[x].z, codes[x].w};
-                // Features behind d_in: their column of G is zero and so is their code.  Four entries at a time, each into sums of its own, so that
-                // their loads, additions and stores overlap: one after the other 128 of them took 4500 clocks.
+                // Features behind d_in have code 0 and a column of zeros, but NaN where dZ is infinite: nothing of them is added to level 0.
+                const int left = p.d_in - (u.f0 + half * 128 + 32 * x);
+                if (left < 32) {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) acc[e] = e < left ? acc[e] : 0u;
+                }
+                // Four entries at a time, each into sums of its own, so that their loads, additions and stores overlap: one after the other 128 of
+                // them took 4500 clocks.
 #pragma unroll
                 for (int e = 0; e < 32; e += LG_SETS) {
                     float v[LG_SETS];

@@ -49,3 +49,25 @@ def test_slope_of_every_value(dev, dtype, act):
         z = Z.double()
         slope = torch.where(z < -800.0, 0.0, torch.where(z > 800.0, 1.0, slope64(z.clamp(-800.0, 800.0), act)))
         within(dZ, size * slope, rounded(size * slope, abs(size) * slope_tolerance(z, act), DT[dtype]))
+
+
+@pytest.mark.parametrize("d_in", [264, 8, 128])
+def test_infinite_gradients_leave_unused_levels_alone(dev, d_in):
+    """A level that no weight has gets no gradient, an infinite dZ in its channel or not: nothing of what fills a tile up reaches it."""
+    n, d_out, m = 6, 40, 4
+    gen, Q, codebook, codes, table, W = layer(dev, d_in, d_out, m, torch.float16, 2)
+    Q.clamp_min_(1)                                       # the code of the padding; no weight has it
+    Q[:, 0], Q[:, 1] = 1, 2
+    Q[:, 2:][Q[:, 2:] == 3] = 1                           # nor level 3
+    codes, table = libgq.gq_linear_pack(Q, codebook, torch.float16)
+    X = torch.rand(n, d_in, generator=gen, device=dev).add_(0.5).half()
+    dY = torch.randn(n, d_out, generator=gen, device=dev).half()
+    ws = libgq.alloc_workspace(libgq.gq_linear_grad_workspace_bytes(n, d_in, d_out), dev)
+    want = libgq.gq_linear_grad(dY, X, codes, table, m, ws, need_x=False)
+    dY[2, 7], dY[4, 30] = float("inf"), float("-inf")
+    got = libgq.gq_linear_grad(dY, X, codes, table, m, ws, need_x=False)
+    libgq.gq_check()
+    for j, value in ((7, float("inf")), (30, float("-inf"))):
+        assert got[2][j].tolist() == [0.0, value, value, 0.0] and float(got[3][j]) == value
+    rest = [j for j in range(d_out) if j not in (7, 30)]
+    assert torch.equal(got[2][rest], want[2][rest]) and torch.equal(got[3][rest], want[3][rest])
