@@ -526,8 +526,9 @@ enum gq_kernel_id {
  * was recorded so far, so a caller can time a sample of its launches (the event pairs cost about 4 % of a
  * step of 52 launches when every launch is timed).  gq_kernel_timing_read() waits for the recorded events and writes, per
  * gq_kernel_id, the summed device time in milliseconds and the number of launches into two HOST
- * arrays of GQ_KERNEL_COUNT entries, then discards them.  Off by default.
- * gq_kernel_timing_read_all() does the same for the first `count` kernels (1 .. GQ_KERNEL_COUNT_ALL; arrays of `count` entries).
+ * arrays of GQ_KERNEL_COUNT entries, then discards all that was recorded.  Off by default.
+ * gq_kernel_timing_read_all() does the same for the first `count` kernels (1 .. GQ_KERNEL_COUNT_ALL; arrays of `count` entries);
+ * what either call does not report it discards too.
  */
 int32_t gq_kernel_timing_enable(int32_t enable);
 int32_t gq_kernel_timing_read(double *ms_sum, uint64_t *launches);

@@ -1816,7 +1816,7 @@ int32_t gq_kernel_timing_read_all(double *ms_sum, uint64_t *launches, int32_t co
     if (!ms_sum || !launches || count_ids < 1 || count_ids > GQ_KERNEL_COUNT_ALL) return GQ_ERR_INVALID_ARG;
     std::lock_guard<std::mutex> lock(g_timing_mutex);
     int32_t rc = GQ_OK;
-    for (int id = 0; id < count_ids; ++id) {
+    for (int id = 0; id < GQ_KERNEL_COUNT_ALL; ++id) {      // those that are not asked for are discarded as well
         double total = 0.0;
         uint64_t count = 0;
         for (auto &pr : g_timing_events[id]) {
@@ -1834,6 +1834,7 @@ int32_t gq_kernel_timing_read_all(double *ms_sum, uint64_t *launches, int32_t co
             cudaEventDestroy(pr.second);
         }
         g_timing_events[id].clear();
+        if (id >= count_ids) continue;
         ms_sum[id] = total;
         launches[id] = count;
     }
