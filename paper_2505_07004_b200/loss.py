@@ -41,7 +41,7 @@ def token_logprobs(logits: torch.Tensor, targets: torch.Tensor, top: int = 0):
     if logits.shape[:-1] != targets.shape:
         raise ValueError("targets must have the shape of logits without its last dimension")
     rows = logits.reshape(-1, vocab)
-    if vocab > 1 and rows.stride(1) != 1:
+    if (vocab > 1 and rows.stride(1) != 1) or (rows.shape[0] > 1 and rows.stride(0) < vocab):      # (rows that share memory: expanded ones)
         rows = rows.contiguous()
     logp, entropy, top_logp, top_ids = _TokenLogprobs.apply(rows, targets.reshape(-1).contiguous(), int(top))
     shape = targets.shape
