@@ -83,6 +83,13 @@ class QuantizedLinear(torch.nn.Module):
         self.pre_activation_hooks = {}
         self._next_hook = 0
 
+    def _apply(self, fn, recurse=True):
+        """Module.to, .half() and their like move the layer, but do not cast it: levels, bias and codebook belong to ``dtype``."""
+        def move(t):
+            moved = fn(t)
+            return moved if moved.dtype == t.dtype else t.to(moved.device)
+        return super()._apply(move, recurse)
+
     def make_table(self, codebook: torch.Tensor) -> torch.Tensor:
         table = torch.zeros((self.d_out, 16), dtype=self.dtype, device=codebook.device)
         table[:, :self.m] = codebook.detach()
