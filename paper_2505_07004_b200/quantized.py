@@ -33,7 +33,7 @@ class _QuantizedLinear(torch.autograd.Function):
             ctx.layer = layer
             ctx.shapes = x.shape, x.dtype, None if residual is None else (residual.shape, residual.dtype), None if bias is None else bias.dtype
             ctx.save_for_backward(X, table, Z)
-        return Y.view(*x.shape[:-1], layer.d_out)
+        return Y.view(*x.shape[:-1], layer.d_out).to(layer.out_dtype)
 
     @staticmethod
     @once_differentiable
@@ -68,14 +68,16 @@ class QuantizedLinear(torch.nn.Module):
 
     ``Q`` (uint8 ``[d_out, d_in]``) and ``codebook`` (fp32 ``[d_out, m]``) as gq_lnq leaves them; activations, bias and residual are computed
     with in ``dtype`` (bfloat16 or float16), to which the levels are rounded.  Without ``train_levels`` the layout is made once; with it the
-    levels are a parameter, rounded at every forward pass, and get a gradient (the codes stay)."""
+    levels are a parameter, rounded at every forward pass, and get a gradient (the codes stay).  Inputs may have any floating type; outputs
+    have ``out_dtype`` (``dtype`` unless given), which is all that Module.to(dtype) and its like change: levels and bias keep theirs."""
 
     def __init__(self, Q: torch.Tensor, codebook: torch.Tensor, bias: Optional[torch.Tensor] = None, activation: int = api.GQ_ACT_NONE,
-                 dtype=torch.bfloat16, train_levels: bool = False):
+                 dtype=torch.bfloat16, train_levels: bool = False, out_dtype: Optional[torch.dtype] = None):
         super().__init__()
         codes, table = api.gq_linear_pack(Q.contiguous(), codebook.float().contiguous(), dtype)
         self.d_out, self.d_in = int(Q.shape[0]), int(Q.shape[1])
         self.m, self.activation, self.dtype = int(codebook.shape[1]), int(activation), dtype
+        self.out_dtype = dtype if out_dtype is None else out_dtype
         self.register_buffer("codes", codes)
         self.register_buffer("table", None if train_levels else table)
         self.codebook = torch.nn.Parameter(codebook.detach().float().clone()) if train_levels else None
@@ -84,11 +86,15 @@ class QuantizedLinear(torch.nn.Module):
         self._next_hook = 0
 
     def _apply(self, fn, recurse=True):
-        """Module.to, .half() and their like move the layer, but do not cast it: levels, bias and codebook belong to ``dtype``."""
+        """Module.to, .half() and their like move the layer, but do not cast it: levels, bias and codebook belong to ``dtype``.  The type
+        of its outputs follows the model's."""
         def move(t):
             moved = fn(t)
             return moved if moved.dtype == t.dtype else t.to(moved.device)
-        return super()._apply(move, recurse)
+        out_dtype = fn(torch.empty(0, dtype=self.out_dtype, device=self.codes.device)).dtype
+        super()._apply(move, recurse)
+        self.out_dtype = out_dtype
+        return self
 
     def make_table(self, codebook: torch.Tensor) -> torch.Tensor:
         table = torch.zeros((self.d_out, 16), dtype=self.dtype, device=codebook.device)
@@ -117,7 +123,8 @@ class QuantizedLinear(torch.nn.Module):
 def quantise(linear: torch.nn.Linear, H: torch.Tensor, m: int = 16, T: int = 2, K: int = 4, dtype=torch.bfloat16, train_levels: bool = False,
              activation: int = api.GQ_ACT_NONE) -> QuantizedLinear:
     """Algorithm 2 on a layer's weights with its guided Hessians (``[g, d_in, d_in]`` from ``GuidedHessianCapture``), started from ``m``
-    equally spaced levels per channel, and the layer that computes with the result."""
+    equally spaced levels per channel, and the layer that computes with the result.  Its outputs have the type of the layer's weights, so
+    that the layers behind it find what they did."""
     W = linear.weight.detach().float().contiguous()
     lo, hi = W.amin(1, keepdim=True), W.amax(1, keepdim=True)
     step = (hi - lo) / max(m - 1, 1)
@@ -125,4 +132,4 @@ def quantise(linear: torch.nn.Linear, H: torch.Tensor, m: int = 16, T: int = 2, 
     Q = Q.clamp_(0, m - 1).to(torch.uint8)
     workspace = api.alloc_workspace(api.gq_lnq_workspace_bytes(W.shape[1], W.shape[0], H.shape[0], m), W.device)
     _, Q, codebook = api.gq_lnq(W, Q, m, H, T, K, workspace)
-    return QuantizedLinear(Q, codebook, linear.bias, activation, dtype, train_levels)
+    return QuantizedLinear(Q, codebook, linear.bias, activation, dtype, train_levels, linear.weight.dtype)

@@ -5,7 +5,9 @@ import pytest
 import torch
 
 from paper_2505_07004_b200 import api as libgq
-from paper_2505_07004_b200.quantized import QuantizedLinear
+from paper_2505_07004_b200.capture import GuidedHessianCapture
+from paper_2505_07004_b200.loss import end_loss
+from paper_2505_07004_b200.quantized import QuantizedLinear, quantise
 
 pytestmark = pytest.mark.gpu
 
@@ -48,4 +50,39 @@ def test_casting_a_model_leaves_the_layer_its_numbers(dev, dtype, train_levels, 
     y = x.clone().requires_grad_()
     model(y).float().sum().backward()
     assert y.grad.dtype == dtype and bool(y.grad.isfinite().all())
+    libgq.gq_check()
+
+
+class Net(torch.nn.Module):
+    def __init__(self):
+        super().__init__()
+        self.embed = torch.nn.Embedding(96, 64)
+        self.up = torch.nn.Linear(64, 128)
+        self.down = torch.nn.Linear(128, 64, bias=False)
+        self.head = torch.nn.Linear(64, 96, bias=False)
+
+    def forward(self, ids):
+        h = self.embed(ids)
+        return self.head(h + self.down(torch.nn.functional.silu(self.up(h))))
+
+
+@pytest.mark.parametrize("model_dtype", [torch.float32, torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("layer_dtype", [torch.bfloat16, torch.float16])
+def test_layers_of_a_model_of_another_type(dev, model_dtype, layer_dtype):
+    """A layer that takes a torch.nn.Linear's place returns that layer's type, so that the layers behind it find what they did."""
+    torch.manual_seed(1)
+    net = Net().to(dev)
+    batches = [(torch.randint(0, 96, (2, 33), device=dev), torch.randint(0, 96, (2, 33), device=dev))]
+    H = GuidedHessianCapture({"up": net.up, "down": net.down}, 2).calibrate(net, batches)
+    net = net.to(model_dtype)
+    for name in ("up", "down"):
+        setattr(net, name, quantise(getattr(net, name), H[name], dtype=layer_dtype))
+    logits = net(batches[0][0])
+    assert logits.dtype == model_dtype and net.up(net.embed(batches[0][0])).dtype == model_dtype
+    end_loss(logits, batches[0][1]).backward()
+    assert net.embed.weight.grad.dtype == model_dtype and bool(net.embed.weight.grad.isfinite().all())
+    for other in (torch.float32, torch.bfloat16):         # and follows the model
+        assert net.to(other)(batches[0][0]).dtype == other
+    assert QuantizedLinear(torch.zeros(8, 8, dtype=torch.uint8, device=dev), torch.zeros(8, 4, device=dev), dtype=layer_dtype)(
+        torch.zeros(1, 8, device=dev)).dtype == layer_dtype      # by itself: its own type
     libgq.gq_check()
