@@ -801,17 +801,29 @@ def gq_linear_grad_workspace_bytes(n: int, d_in: int, d_out: int) -> int:
     return int(lib().gq_linear_grad_workspace_bytes(n, d_in, d_out))
 
 
-def gq_linear_grad(dY: torch.Tensor, X: torch.Tensor, codes: torch.Tensor, table: torch.Tensor, m: int, workspace: Optional[torch.Tensor] = None,
+def gq_linear_grad(dY: torch.Tensor, X: Optional[torch.Tensor], codes: torch.Tensor, table: torch.Tensor, m: int, workspace: Optional[torch.Tensor] = None,
                    Z: Optional[torch.Tensor] = None, activation: int = GQ_ACT_NONE, need_x: bool = True, need_table: bool = True,
-                   need_bias: bool = True, dZ: Optional[torch.Tensor] = None, dX: Optional[torch.Tensor] = None, stream=None):
+                   need_bias: bool = True, dZ: Optional[torch.Tensor] = None, dX: Optional[torch.Tensor] = None, stream=None, d_in: Optional[int] = None):
     """Backward pass of :func:`gq_linear`: ``(dZ, dX, d_table, d_bias)``.  ``dZ`` (the gradient of the pre-activation, what
     :func:`gq_saliency` reduces) is ``dY`` itself without an activation; ``d_table`` (fp32 ``[d_out, m]``) and ``d_bias`` (fp32 ``[d_out]``)
-    need the workspace.  What is not needed comes back as ``None``."""
-    n, d_in, ld_x = _rows(X, "X")
-    d_out, code = _linear_weights(X, codes, table, d_in)
-    dtype, dev = X.dtype, X.device
+    need the workspace.  What is not needed comes back as ``None``.  ``X`` is read for ``d_table`` only: without it the call takes ``None`` and
+    the number of features ``d_in``."""
+    if X is not None:
+        n, width, ld_x = _rows(X, "X")
+        if d_in is not None and d_in != width:
+            raise ValueError("d_in is %d but X has %d features" % (d_in, width))
+        d_in, x_ptr, like = width, X.data_ptr(), X
+        names, tensors = ("dY", "X", "codes", "table"), (dY, X, codes, table)
+    else:
+        if need_table:
+            raise ValueError("the gradient of the levels needs X")
+        if d_in is None:
+            raise ValueError("without X the call needs d_in")
+        (n, _, _), x_ptr, ld_x, like = _rows(dY, "dY"), 0, 0, dY
+        names, tensors = ("dY", "codes", "table"), (dY, codes, table)
+    d_out, code = _linear_weights(like, codes, table, d_in)
+    dtype, dev = like.dtype, like.device
     dy_ptr, ld_dy = _matrix(dY, (n, d_out), dtype, "dY")
-    names, tensors = ("dY", "X", "codes", "table"), (dY, X, codes, table)
     z_ptr = ld_z = dz_ptr = ld_dz = dx_ptr = ld_dx = dt_ptr = db_ptr = ws_ptr = ws_bytes = 0
     d_table = d_bias = None
     if Z is not None:
@@ -841,6 +853,6 @@ def gq_linear_grad(dY: torch.Tensor, X: torch.Tensor, codes: torch.Tensor, table
         ws_ptr, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
         names, tensors = names + ("workspace",), tensors + (workspace,)
     _call("gq_linear_grad",
-          (dy_ptr, code, n, d_out, ld_dy, z_ptr, ld_z, activation, X.data_ptr(), d_in, ld_x, codes.data_ptr(), table.data_ptr(), m, dz_ptr, ld_dz,
+          (dy_ptr, code, n, d_out, ld_dy, z_ptr, ld_z, activation, x_ptr, d_in, ld_x, codes.data_ptr(), table.data_ptr(), m, dz_ptr, ld_dz,
            dx_ptr, ld_dx, dt_ptr, db_ptr, ws_ptr, ws_bytes), stream, names, tensors)
     return (dY if activation == GQ_ACT_NONE else dZ), dX, d_table, d_bias

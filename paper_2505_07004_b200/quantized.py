@@ -32,7 +32,7 @@ class _QuantizedLinear(torch.autograd.Function):
         if keep:
             ctx.layer = layer
             ctx.shapes = x.shape, x.dtype, None if residual is None else (residual.shape, residual.dtype), None if bias is None else bias.dtype
-            ctx.save_for_backward(X, table, Z)
+            ctx.save_for_backward(X if ctx.needs_input_grad[1] else None, table, Z)      # (only the levels' gradient reads X)
         return Y.view(*x.shape[:-1], layer.d_out).to(layer.out_dtype)
 
     @staticmethod
@@ -44,9 +44,9 @@ class _QuantizedLinear(torch.autograd.Function):
         dY = _tokens(grad, layer.dtype)
         workspace = None
         if need_table or need_bias:
-            workspace = api.alloc_workspace(api.gq_linear_grad_workspace_bytes(X.shape[0], X.shape[1], layer.d_out), X.device)
+            workspace = api.alloc_workspace(api.gq_linear_grad_workspace_bytes(dY.shape[0], layer.d_in, layer.d_out), dY.device)
         dZ, dX, d_table, d_bias = api.gq_linear_grad(dY, X, layer.codes, table, layer.m, workspace, Z=Z, activation=layer.activation,
-                                                     need_x=need_x, need_table=need_table, need_bias=need_bias)
+                                                     need_x=need_x, need_table=need_table, need_bias=need_bias, d_in=layer.d_in)
         for hook in list(layer.pre_activation_hooks.values()):
             hook(dZ.view(*shape[:-1], layer.d_out))
         if dX is not None:

@@ -86,3 +86,44 @@ def test_layers_of_a_model_of_another_type(dev, model_dtype, layer_dtype):
     assert QuantizedLinear(torch.zeros(8, 8, dtype=torch.uint8, device=dev), torch.zeros(8, 4, device=dev), dtype=layer_dtype)(
         torch.zeros(1, 8, device=dev)).dtype == layer_dtype      # by itself: its own type
     libgq.gq_check()
+
+
+@pytest.mark.parametrize("train_levels", [False, True])
+@pytest.mark.parametrize("act", [libgq.GQ_ACT_NONE, libgq.GQ_ACT_GELU])
+def test_inputs_are_kept_only_for_the_levels_gradient(dev, train_levels, act):
+    layer = make(dev, train_levels=train_levels, act=act)
+    layer.bias.requires_grad_(True)
+    x = torch.randn(3, 5, 72, device=dev).bfloat16().requires_grad_()
+    kept = []
+    with torch.autograd.graph.saved_tensors_hooks(lambda t: kept.append(tuple(t.shape)) or t, lambda t: t):
+        y = layer(x)
+    assert ((15, 72) in kept) == train_levels and ((15, 40) in kept) == (act != libgq.GQ_ACT_NONE)
+    y.backward(torch.ones_like(y))
+    # the same gradients from the call itself, which is given X
+    dY, X = torch.ones(15, 40, device=dev).bfloat16(), x.detach().view(15, 72)
+    table = layer.table if not train_levels else layer.make_table(layer.codebook)
+    Z = torch.empty_like(dY) if act != libgq.GQ_ACT_NONE else None
+    libgq.gq_linear(X, layer.codes, table, layer.m, bias=layer.bias.detach(), activation=act, Z=Z)
+    ws = libgq.alloc_workspace(libgq.gq_linear_grad_workspace_bytes(15, 72, 40), dev)
+    _, dX, d_table, d_bias = libgq.gq_linear_grad(dY, X, layer.codes, table, layer.m, ws, Z=Z, activation=act)
+    assert torch.equal(x.grad.view(15, 72), dX) and torch.equal(layer.bias.grad, d_bias.bfloat16())
+    assert not train_levels or torch.equal(layer.codebook.grad, d_table)
+    without = libgq.gq_linear_grad(dY, None, layer.codes, table, layer.m, ws, Z=Z, activation=act, need_table=False, d_in=72)
+    assert torch.equal(without[1], dX) and without[2] is None and torch.equal(without[3], d_bias)
+    libgq.gq_check()
+
+
+def test_gradients_without_inputs_refuse(dev):
+    layer = make(dev)
+    dY = torch.ones(3, 40, device=dev).bfloat16()
+    ws = libgq.alloc_workspace(libgq.gq_linear_grad_workspace_bytes(3, 72, 40), dev)
+    with pytest.raises(ValueError, match="X"):
+        libgq.gq_linear_grad(dY, None, layer.codes, layer.table, 16, ws, d_in=72)
+    with pytest.raises(ValueError, match="d_in"):
+        libgq.gq_linear_grad(dY, None, layer.codes, layer.table, 16, ws, need_table=False)
+    with pytest.raises(ValueError, match="d_in"):
+        libgq.gq_linear_grad(dY, torch.ones(3, 72, device=dev).bfloat16(), layer.codes, layer.table, 16, ws, d_in=80)
+    with pytest.raises(ValueError, match="codes"):
+        libgq.gq_linear_grad(dY, None, layer.codes, layer.table, 16, ws, need_table=False, d_in=104)
+    with pytest.raises(ValueError, match="table"):
+        libgq.gq_linear_grad(dY.half(), None, layer.codes, layer.table, 16, ws, need_table=False, d_in=72)
