@@ -22,11 +22,11 @@ def _tokens(t: torch.Tensor, dtype) -> torch.Tensor:
 
 class _QuantizedLinear(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, codebook, bias, residual, _anchor, layer):
+    def forward(ctx, x, codebook, bias, residual, _anchor, layer, graph):
         X = _tokens(x, layer.dtype)
         table = layer.table if layer.table is not None else layer.make_table(codebook)
         R = _tokens(residual, layer.dtype) if residual is not None else None
-        keep = any(ctx.needs_input_grad)
+        keep = graph and any(ctx.needs_input_grad)           # (an input may require a gradient that no graph is made for)
         Z = X.new_empty((X.shape[0], layer.d_out)) if keep and layer.activation != api.GQ_ACT_NONE else None
         Y = api.gq_linear(X, layer.codes, table, layer.m, bias=bias, activation=layer.activation, residual=R, Z=Z)
         if keep:
@@ -52,7 +52,7 @@ class _QuantizedLinear(torch.autograd.Function):
         if dX is not None:
             dX = dX.view(shape).to(dtype)
         d_residual = grad.reshape(residual[0]).to(residual[1]) if need_residual else None
-        return dX, d_table, d_bias.to(bias_dtype) if need_bias else None, d_residual, None, None
+        return dX, d_table, d_bias.to(bias_dtype) if need_bias else None, d_residual, None, None, None
 
 
 class _Handle:
@@ -113,8 +113,9 @@ class QuantizedLinear(torch.nn.Module):
         if x.shape[-1] != self.d_in:
             raise ValueError("the layer takes %d features, not %d" % (self.d_in, x.shape[-1]))
         # hooks want the gradient even where nothing below the layer does: something that requires one keeps it in the graph
-        anchor = torch.empty(0, device=x.device, requires_grad=True) if self.pre_activation_hooks and torch.is_grad_enabled() else None
-        return _QuantizedLinear.apply(x, self.codebook, self.bias, residual, anchor, self)
+        graph = torch.is_grad_enabled()
+        anchor = torch.empty(0, device=x.device, requires_grad=True) if self.pre_activation_hooks and graph else None
+        return _QuantizedLinear.apply(x, self.codebook, self.bias, residual, anchor, self, graph)
 
     def extra_repr(self) -> str:
         return "d_in=%d, d_out=%d, m=%d, activation=%d, dtype=%s" % (self.d_in, self.d_out, self.m, self.activation, self.dtype)

@@ -127,3 +127,18 @@ def test_gradients_without_inputs_refuse(dev):
         libgq.gq_linear_grad(dY, None, layer.codes, layer.table, 16, ws, need_table=False, d_in=104)
     with pytest.raises(ValueError, match="table"):
         libgq.gq_linear_grad(dY.half(), None, layer.codes, layer.table, 16, ws, need_table=False, d_in=72)
+
+
+def test_no_pre_activation_without_a_graph(dev, monkeypatch):
+    """An evaluation under no_grad neither allocates nor writes what only a backward pass reads."""
+    layer = make(dev, train_levels=True)
+    x = torch.randn(6, 72, device=dev).bfloat16().requires_grad_()
+    given, call = [], libgq.gq_linear
+    monkeypatch.setattr(libgq, "gq_linear", lambda *a, **k: given.append(k.get("Z")) or call(*a, **k))
+    want = layer(x)
+    with torch.no_grad():
+        got = layer(x)
+    with torch.inference_mode():
+        again = layer(x.detach())
+    assert given[0] is not None and given[1] is None and given[2] is None
+    assert torch.equal(got, want) and torch.equal(again, want) and not got.requires_grad
