@@ -98,7 +98,10 @@ class GuidedHessianCapture:
 
     def calibrate(self, model, batches) -> Dict[str, torch.Tensor]:
         """Both passes over ``(inputs, targets)`` batches with the end loss of ``model(inputs)`` (logits ``[..., vocab]``), then finalize.
-        Gradients that the backward passes leave in the parameters are dropped."""
+        Batches of an iterator, which can be gone through once, are kept for the second pass.  Gradients that the backward passes leave in
+        the parameters are dropped."""
+        if iter(batches) is batches:
+            batches = list(batches)
         with self.saliency_pass():
             for inputs, targets in batches:
                 end_loss(model(inputs), targets).backward()
@@ -109,10 +112,10 @@ class GuidedHessianCapture:
         return self.finalize()
 
     def finalize(self) -> Dict[str, torch.Tensor]:
-        for name, H in self.H.items():
-            if self._next.get(name, 0) != len(self.s[name]):
-                raise RuntimeError("layer %s: %d saliency blocks but %d forward calls"
-                                   % (name, len(self.s[name]), self._next.get(name, 0)))
+        for name, blocks in self.s.items():
+            if self._next.get(name, 0) != len(blocks):
+                raise RuntimeError("layer %s: %d saliency blocks but %d forward calls" % (name, len(blocks), self._next.get(name, 0)))
+        for H in self.H.values():
             api.gq_hessian_finalize(H)
         api.gq_check()
         return self.H

@@ -142,3 +142,33 @@ def test_no_pre_activation_without_a_graph(dev, monkeypatch):
         again = layer(x.detach())
     assert given[0] is not None and given[1] is None and given[2] is None
     assert torch.equal(got, want) and torch.equal(again, want) and not got.requires_grad
+
+
+def test_calibration_on_an_iterator(dev):
+    """Both passes see the batches of a generator too."""
+    torch.manual_seed(2)
+    net = Net().to(dev).bfloat16()
+    batches = [(torch.randint(0, 96, (b, 17), device=dev), torch.randint(0, 96, (b, 17), device=dev)) for b in (3, 2, 1)]
+    names = ("up", "down")
+    want = GuidedHessianCapture({k: getattr(net, k) for k in names}, 4).calibrate(net, batches)
+    for once in (iter(batches), (b for b in batches), zip([b[0] for b in batches], [b[1] for b in batches])):
+        got = GuidedHessianCapture({k: getattr(net, k) for k in names}, 4).calibrate(net, once)
+        assert set(got) == set(names)
+        for k in names:
+            # sums over the batches' tokens in the same order, but for the order of two writers of a tile
+            assert bool(((got[k] - want[k]).abs() <= 2.0 ** -16 * want[k].diagonal(dim1=1, dim2=2).amax(1)[:, None, None]).all())
+
+
+def test_a_layer_without_a_forward_pass_is_an_error(dev):
+    torch.manual_seed(2)
+    net = Net().to(dev).bfloat16()
+    cap = GuidedHessianCapture({"up": net.up, "down": net.down}, 4)
+    ids, targets = torch.randint(0, 96, (2, 17), device=dev), torch.randint(0, 96, (2, 17), device=dev)
+    with cap.saliency_pass():
+        end_loss(net(ids), targets).backward()
+    with pytest.raises(RuntimeError, match="saliency blocks but 0 forward calls"):
+        cap.finalize()
+    with cap.hessian_pass(), torch.no_grad():
+        net.up(net.embed(ids))
+    with pytest.raises(RuntimeError, match="down"):
+        cap.finalize()
