@@ -642,6 +642,8 @@ def _empty(shape, stride, dtype, device, stream=None) -> torch.Tensor:
     given a stream of its own gets memory of that stream: what the current stream has still to do with memory that was
     freed on it must not meet the call's outputs."""
     if stream is not None:
+        if not isinstance(stream, torch.cuda.Stream):
+            stream = torch.cuda.ExternalStream(int(stream.cuda_stream), device=device)      # a plain handle, as _stream_ptr takes it
         with torch.cuda.stream(stream):
             return torch.empty_strided(shape, stride, dtype=dtype, device=device)
     return torch.empty_strided(shape, stride, dtype=dtype, device=device)
