@@ -1521,15 +1521,20 @@ static CUtensorMapDataType map_type(int32_t dtype)
     return dtype == GQ_DTYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
 }
 
-// The tensor-core product: forward (X [n, d_in] -> [n, d_out]) or backward (dZ [n, d_out] -> [n, d_in]).
+// Tiles of 256 x 512 of a tensor-core product with `rows` rows on the weights' side.
+static int64_t linear_tiles(int64_t rows, int64_t n)
+{
+    return (rows + gq::TILE_M - 1) / gq::TILE_M * ((n + gq::LP_HALVES * gq::TILE_N - 1) / (gq::LP_HALVES * gq::TILE_N));
+}
+constexpr int64_t kLinearMaxTiles = (1ll << 29) - 1;
+
+// The tensor-core product: forward (X [n, d_in] -> [n, d_out]) or backward (dZ [n, d_out] -> [n, d_in]), at most kLinearMaxTiles tiles.
 static int32_t linear_pair(bool back, gq::LinearParams p, int32_t dtype, const void *in, int64_t ld_in, int32_t m, DeviceInfo *di, cudaStream_t st)
 {
     const int rows = back ? p.d_in : p.d_out, kdim = back ? p.d_out : p.d_in;
-    const int64_t row_tiles = (rows + gq::TILE_M - 1) / gq::TILE_M;
-    const int64_t tok_tiles = (p.n + gq::LP_HALVES * gq::TILE_N - 1) / (gq::LP_HALVES * gq::TILE_N), tiles = row_tiles * tok_tiles;
-    if (tiles >= (1ll << 29)) return GQ_ERR_UNSUPPORTED_SHAPE;
+    const int64_t row_tiles = (rows + gq::TILE_M - 1) / gq::TILE_M, tiles = linear_tiles(rows, p.n);
     p.row_tiles = static_cast<int>(row_tiles);
-    p.tok_tiles = static_cast<int>(tok_tiles);
+    p.tok_tiles = static_cast<int>(tiles / row_tiles);
     // Whole tiles (two halves on one looked-up operand) in full rounds; the last round as halves where there are pairs for all of them.
     const int rest = static_cast<int>(tiles % di->max_pairs);
     p.doubles = static_cast<int>(2 * rest <= di->max_pairs && p.n > gq::TILE_N ? tiles - rest : tiles);
@@ -1575,6 +1580,7 @@ int32_t gq_linear(const void *X, int32_t dtype, int64_t n, int64_t d_in, int64_t
 {
     if (int32_t rc = check_linear_shape(dtype, n, d_in, d_out, m)) return rc;
     if (activation < GQ_ACT_NONE || activation > GQ_ACT_GELU) return GQ_ERR_INVALID_ARG;
+    if (linear_tiles(d_out, n) > kLinearMaxTiles) return GQ_ERR_UNSUPPORTED_SHAPE;
     if (n == 0) return GQ_OK;
     if (!codes || !table) return GQ_ERR_INVALID_ARG;
     if (int32_t rc = check_rows16(X, d_in, ld_x)) return rc;
@@ -1682,6 +1688,9 @@ int32_t gq_linear_grad(const void *dY, int32_t dtype, int64_t n, int64_t d_out, 
     if (int32_t rc = check_linear_shape(dtype, n, d_in, d_out, m)) return rc;
     if (activation < GQ_ACT_NONE || activation > GQ_ACT_GELU) return GQ_ERR_INVALID_ARG;
     const bool has_act = activation != GQ_ACT_NONE;
+    const LevelGradPlan P = level_grad_plan(n, d_in, d_out);
+    const int64_t per_tile = P.f_tiles * P.chunks, units = P.ch_tiles * per_tile;
+    if ((dX && linear_tiles(d_in, n) > kLinearMaxTiles) || (d_table && units >= (1ll << 40))) return GQ_ERR_UNSUPPORTED_SHAPE;
     const size_t table_out = d_table ? static_cast<size_t>(d_out) * m * 4 : 0, bias_out = d_bias ? static_cast<size_t>(d_out) * 4 : 0;
     if (!aligned(d_table, 4) || !aligned(d_bias, 4)) return GQ_ERR_ALIGNMENT;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -1745,9 +1754,6 @@ int32_t gq_linear_grad(const void *dY, int32_t dtype, int64_t n, int64_t d_out, 
         p.ld_out = ld_dx;
         if (int32_t rc = linear_pair(true, p, dtype, grad, ld_grad, m, di, st)) return rc;
     }
-    const LevelGradPlan P = level_grad_plan(n, d_in, d_out);
-    const int64_t per_tile = P.f_tiles * P.chunks, units = P.ch_tiles * per_tile;
-    if (units >= (1ll << 40)) return GQ_ERR_UNSUPPORTED_SHAPE;
     int pairs = di->max_pairs < kLevelGradPairs ? di->max_pairs : kLevelGradPairs;
     if (units < pairs) pairs = static_cast<int>(units);
     if (d_table) {
