@@ -111,8 +111,10 @@ struct LevelPlanes {
     }
 };
 
-// The activation of N values.  The kind is asked for once: a branch per value keeps the values' evaluations from overlapping, and the
-// epilogue of 2048 tokens 4096 -> 11008 took 46 us longer with SiLU than without.
+// The activation of N values, each about to be rounded to 16 bits.  SiLU by the fast exponential and quotient: 2 + 1.2 |z| units in the last
+// place, and 0 below z = -87.3, where a divisor above 2^126 makes the quotient 0 (the value is smaller than |z| 2^-126).  The kind is asked
+// for once: a branch per value keeps the values' evaluations from overlapping, and the epilogue of 2048 tokens 4096 -> 11008 took 46 us
+// longer with SiLU than without.
 template <int N>
 __device__ __forceinline__ void activate(float (&z)[N], int act)
 {
