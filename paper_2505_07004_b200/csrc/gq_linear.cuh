@@ -132,8 +132,9 @@ __device__ __forceinline__ void activate(float (&z)[N], int act)
 // The slope's fp32 value decides how dZ is rounded, and the fp32 gradients are those of the rounded dZ: no fast approximations.
 // SiLU: s (1 + z (1 - s)) with s = 1 / (1 + exp(-z)).  Below z = -64 s is exp(z) to the last bit, down to 0, where a reciprocal of exp(-z) would
 // have to stop at infinity; above, d = 1 + exp(-z) lies in [1, 2^93], and one Newton-Raphson step r + r (1 - d r) takes the fast quotient's
-// two units in the last place to half of one and a little.  The slope is good to 24 times 2^-24 of s (1 + |z| (1 - s)).  (dZ of 2048 x 4096: 16.2 us; with
-// __frcp_rn, which branches, 17.3; with the quotient alone 14.9, but up to twice as many of them are rounded the other way.)
+// two units in the last place to half of one and a little.  The slope is good to 24 times 2^-24 of s (1 + |z| (1 - s)).  dZ of 2048 x 4096
+// takes 16.2 us; with __frcp_rn, which branches, 17.3; with the quotient alone 14.9, but up to twice as many of them are rounded the
+// other way.
 __device__ __forceinline__ float activation_slope(float z, int act)
 {
     if (act == LIN_RELU) return z > 0.0f ? 1.0f : 0.0f;
